@@ -311,6 +311,95 @@ int rkv_append_kernel_of(const rkv_cache* cache);
  * rkv_quantize_append around its quantize kernel.  Pass NULLs to clear. */
 int rkv_set_profile_events(rkv_cache* cache, void* ev_start, void* ev_stop);
 
+/* ---- a cache in pages ------------------------------------------------------------------------ */
+
+/* A cache whose memory is handed out in pages of `page_tokens` tokens, for servers that admit, extend and
+ * drop sequences all the time and share prefixes: the pool, the page tables and the lengths belong to the
+ * caller, and the library keeps nothing between calls.  It holds keys and values as attention is to see them
+ * (keys with RoPE or any other position code applied) in 16 bits, or quantised as they are written:
+ * blocks of 32 channels of a token's head share a power of two, 8-bit codes are E4M3 and 4-bit codes E2M1
+ * floating-point numbers.  Every number that a cache holds is one of its type (fp16 or bf16).
+ *
+ * Quantisation of a block x[0..31] with largest magnitude A, M the format's largest number (448 / 6):
+ *   e     = the smallest exponent >= e_min with A <= M 2^e; e_min is -15 (fp16) or -118 (bf16) with 8 bits,
+ *           -23 or -126 with 4, which keeps the smallest code a number of the type
+ *   code  = x 2^-e rounded to the nearest number of the format, ties to even; |x| beyond the largest number
+ *           that the format and the type share (1.875 2^15 or 1.875 2^127 with 8 bits, 1.5 2^15 or 1.5 2^127
+ *           with 4) counts as that
+ *   scale = the byte e + 127; 255 for a block that holds an infinity or a NaN, all of which reads as NaN.
+ * Pool: for every page, for every KV head: [page_tokens][head_dim] key codes, the same of value codes, then
+ * (8 and 4 bits) [page_tokens][head_dim / 32] scale bytes of the keys and the same of the values; two
+ * 4-bit codes a byte, the even channel in the low half. */
+typedef struct rkv_paged_config {
+  int32_t n_q_heads;    /* multiple of n_kv_heads; query head h reads KV head h / (n_q_heads / n_kv_heads) */
+  int32_t n_kv_heads;   /* 1..256                                                                 */
+  int32_t head_dim;     /* 64 or 128                                                              */
+  int32_t page_tokens;  /* 16, 32, 64, 128 or 256                                                 */
+  int32_t n_pages;      /* pages of the pool, >= 1                                                */
+  int32_t bits;         /* 16, 8 or 4                                                             */
+  int32_t dtype;        /* of keys, values, queries and outputs: 0 fp16, 1 bf16                   */
+} rkv_paged_config;
+
+/* The sequences that take part in a call and their new rows.  Rows of all sequences are packed: sequence b
+ * owns rows row_start[b] .. row_start[b + 1] - 1 of the tensors, which are its LAST tokens: of lengths[b]
+ * tokens, the new ones included, row row_start[b] + i is the token at position
+ * lengths[b] - (row_start[b + 1] - row_start[b]) + i.  Token t of a sequence is in slot t % page_tokens of
+ * page page_table[b][t / page_tokens].  Rows that no sequence owns are left as they are.
+ * The device arrays are read by the kernels, so that a captured call follows them on every replay; the host's
+ * bounds choose the launch.  Where the arrays contradict the bounds nothing is read or written out of place:
+ *   - a sequence with more rows than max_new or a length outside 0..max_len is not appended to, and what is
+ *     read of it and its attention are NaN;
+ *   - a token whose page number is outside 0..n_pages - 1 is not written and reads as NaN, as does the
+ *     attention of every row that sees it;
+ *   - a row in front of its sequence's first token (more rows than tokens) is not written, reads as zero and
+ *     sees nothing. */
+typedef struct rkv_paged_batch {
+  const int32_t* dev_page_table;  /* [n_seqs][max_pages]; entries behind a sequence's last token are not used */
+  const int32_t* dev_row_start;   /* [n_seqs + 1], ascending from >= 0 to <= n_rows                */
+  const int32_t* dev_lengths;     /* [n_seqs]                                                      */
+  int32_t n_seqs;                 /* 1..65536                                                      */
+  int32_t max_pages;              /* entries of a row of the page table                            */
+  int32_t n_rows;                 /* rows of the packed tensors (0: the call does nothing)         */
+  int32_t max_new;                /* no sequence has more rows than this, 1..n_rows                */
+  int32_t max_len;                /* nor is one longer than this, 1..max_pages * page_tokens       */
+} rkv_paged_batch;
+
+/* Bytes of the pool.  RKV_EINVAL if cfg is unsupported. */
+int rkv_paged_sizes(const rkv_paged_config* cfg, size_t* pool_bytes);
+
+/* Write the rows' keys and values into the pages.
+ *   dev_pool   16-byte aligned, rkv_paged_sizes bytes
+ *   dev_k, dev_v   [n_rows][n_kv_heads][head_dim] of the cache's type, 16-byte aligned; rows lie k_stride /
+ *              v_stride elements apart (a multiple of 8, at least n_kv_heads * head_dim: the two may be
+ *              columns of one projection's output)
+ * Two rows that name the same slot leave either's bytes there. */
+int rkv_paged_append(const rkv_paged_config* cfg, void* dev_pool, const rkv_paged_batch* batch, const void* dev_k, int64_t k_stride,
+                     const void* dev_v, int64_t v_stride, void* stream);
+
+/* Read the rows' keys and values back: the reverse of rkv_paged_append with the same arguments, giving the
+ * numbers that the cache holds.  With as many rows as tokens a whole sequence is read. */
+int rkv_paged_read(const rkv_paged_config* cfg, const void* dev_pool, const rkv_paged_batch* batch, void* dev_k, int64_t k_stride,
+                   void* dev_v, int64_t v_stride, void* stream);
+
+/* Bytes of work space that rkv_paged_attention needs for this batch (0: none). */
+int rkv_paged_scratch(const rkv_paged_config* cfg, const rkv_paged_batch* batch, size_t* scratch_bytes);
+
+/* Attention of the rows over their sequences' cached tokens, themselves included (append them first): chunks
+ * of prompts, drafted tokens, single tokens, in any mixture.  The row at position p sees the tokens t of its
+ * sequence with t <= p (all of them without `causal`) and, with window > 0, t > p - window.
+ *   dev_q      [n_rows][n_q_heads][head_dim] of the cache's type, rows q_stride elements apart (as k_stride)
+ *   scale      of the scores, finite (1 / sqrt(head_dim) by custom)
+ *   dev_out    [n_rows][n_q_heads][head_dim] of the cache's type, dense
+ *   dev_lse    [n_rows][n_q_heads] fp32 log-sum-exp of the scaled scores, or NULL
+ *   dev_scratch  256-byte aligned, scratch_bytes >= what rkv_paged_scratch says for this batch (else
+ *              RKV_EINVAL); calls that may run at the same time need work spaces of their own
+ * A row that sees no token, or whose scores are all -infinity, gets zeros and the log-sum-exp -infinity.
+ * What a row does not see has no influence on it, infinities and NaN included.  Scores, softmax statistics
+ * and sums are held in fp32; the same call on the same data gives the same bits. */
+int rkv_paged_attention(const rkv_paged_config* cfg, const void* dev_pool, const rkv_paged_batch* batch, const void* dev_q,
+                        int64_t q_stride, int32_t causal, int32_t window, float scale, void* dev_out, float* dev_lse,
+                        void* dev_scratch, size_t scratch_bytes, void* stream);
+
 /* ---- test support: exact views of what the cache stores ------------------------------------- */
 
 /* Reconstructed keys and values (Eq. 7, inverse reorder, inverse rotation), original basis, keys

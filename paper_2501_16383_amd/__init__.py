@@ -2,3 +2,4 @@
 from .binding import (  # noqa: F401
     RkvConfig, RkvCache, RkvError, calibrate_perm, fold_rotation, layout_locate, library_path, load_library, query_sizes, select_sinks,
 )
+from .paged import RkvPagedBatch, RkvPagedCache, RkvPagedConfig, paged_sizes  # noqa: F401

@@ -24,6 +24,7 @@ EXPORTS = [
     "rkv_calibrate_perm", "rkv_fold_rotation", "rkv_set_perm", "rkv_select_sinks", "rkv_quantize_append", "rkv_decode_attention", "rkv_decode_attention_static", "rkv_decode_attention_with_current",
     "rkv_decode_attention_multi", "rkv_decode_step", "rkv_quantize_append_ragged", "rkv_cache_lengths", "rkv_cache_truncate",
     "rkv_set_decode_path", "rkv_set_decode_chunk", "rkv_decode_kernel_of", "rkv_append_kernel_of", "rkv_set_profile_events", "rkv_dequantize", "rkv_export_codes", "rkv_import_codes", "rkv_export_sinks", "rkv_layout_locate",
+    "rkv_paged_sizes", "rkv_paged_append", "rkv_paged_read", "rkv_paged_scratch", "rkv_paged_attention",
     "rkv_strerror",
 ]
 
@@ -40,6 +41,15 @@ class _CConfig(C.Structure):
         "batch", "n_q_heads", "n_kv_heads", "head_dim", "max_tokens", "max_sinks", "rot_heads",
         "quant_group", "bits", "perm_span", "rope_style", "v_rotate")] + [
         ("rope_theta", C.c_float), ("clip_ratio", C.c_float), ("keys_rotated", C.c_int32), ("meta_format", C.c_int32)]
+
+
+class _CPagedConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "page_tokens", "n_pages", "bits", "dtype")]
+
+
+class _CPagedBatch(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("dev_page_table", "dev_row_start", "dev_lengths")] + [
+        (n, C.c_int32) for n in ("n_seqs", "max_pages", "n_rows", "max_new", "max_len")]
 
 
 @dataclass
@@ -114,6 +124,12 @@ def load_library():
     lib.rkv_import_codes.argtypes = [vp, i32] + [vp] * 7
     lib.rkv_export_sinks.argtypes = [vp] * 6
     lib.rkv_layout_locate.argtypes = [cfgp, i32, i32, i32, i32, C.POINTER(sz), C.POINTER(i32), C.POINTER(sz)]
+    pagedp, batchp, i64 = C.POINTER(_CPagedConfig), C.POINTER(_CPagedBatch), C.c_int64
+    lib.rkv_paged_sizes.argtypes = [pagedp, C.POINTER(sz)]
+    lib.rkv_paged_append.argtypes = [pagedp, vp, batchp, vp, i64, vp, i64, vp]
+    lib.rkv_paged_read.argtypes = [pagedp, vp, batchp, vp, i64, vp, i64, vp]
+    lib.rkv_paged_scratch.argtypes = [pagedp, batchp, C.POINTER(sz)]
+    lib.rkv_paged_attention.argtypes = [pagedp, vp, batchp, vp, i64, i32, i32, C.c_float, vp, vp, vp, sz, vp]
     lib.rkv_strerror.argtypes = [C.c_int]
     lib.rkv_strerror.restype = C.c_char_p
     for name in EXPORTS:

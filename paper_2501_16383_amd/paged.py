@@ -1,0 +1,139 @@
+"""The cache in pages: ctypes binding of the rkv_paged_* calls.  Argument marshalling only."""
+from __future__ import annotations
+
+import ctypes as C
+from dataclasses import dataclass
+
+from .binding import _check, _CPagedBatch, _CPagedConfig, _dev, _ptr, _stream, load_library
+
+
+@dataclass
+class RkvPagedConfig:
+    """rkv_paged_config: bits 16, 8 (E4M3 codes) or 4 (E2M1 codes); dtype 0 fp16, 1 bf16."""
+    n_q_heads: int
+    n_kv_heads: int
+    n_pages: int
+    head_dim: int = 128
+    page_tokens: int = 64
+    bits: int = 8
+    dtype: int = 0
+
+    def to_c(self) -> _CPagedConfig:
+        return _CPagedConfig(self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_tokens, self.n_pages, self.bits, self.dtype)
+
+
+def paged_sizes(cfg: RkvPagedConfig) -> int:
+    """rkv_paged_sizes: bytes of the pool."""
+    n, cc = C.c_size_t(0), cfg.to_c()
+    _check(load_library().rkv_paged_sizes(C.byref(cc), C.byref(n)), "rkv_paged_sizes")
+    return n.value
+
+
+class RkvPagedBatch:
+    """rkv_paged_batch: the sequences of a call and their new rows.
+
+    page_table [n_seqs, max_pages], row_start [n_seqs + 1] and lengths [n_seqs] are int32 tensors on the device, read by every
+    call anew (and by every replay of a captured one); n_rows, max_new and max_len are the host's bounds on them."""
+
+    def __init__(self, page_table, row_start, lengths, n_rows: int, max_new: int = None, max_len: int = None):
+        import torch
+        if page_table is None or row_start is None or lengths is None:
+            raise TypeError("page_table, row_start and lengths are needed")
+        self.page_table = _dev(page_table, torch.int32, "page_table")
+        self.row_start = _dev(row_start, torch.int32, "row_start")
+        self.lengths = _dev(lengths, torch.int32, "lengths")
+        if page_table.dim() != 2 or row_start.shape != (page_table.shape[0] + 1,) or lengths.shape != page_table.shape[:1]:
+            raise ValueError("page_table must be [n_seqs, max_pages], row_start [n_seqs + 1], lengths [n_seqs]")
+        if row_start.device != page_table.device or lengths.device != page_table.device:
+            raise ValueError("page_table, row_start and lengths must be on one device")
+        self.device = page_table.device
+        self.n_rows, self.max_new, self.max_len = n_rows, max_new, max_len
+
+    def to_c(self, cfg: RkvPagedConfig) -> _CPagedBatch:
+        n_seqs, max_pages = self.page_table.shape
+        return _CPagedBatch(self.page_table.data_ptr(), self.row_start.data_ptr(), self.lengths.data_ptr(), n_seqs, max_pages, self.n_rows,
+                            self.n_rows if self.max_new is None else self.max_new,
+                            min(max_pages * cfg.page_tokens, 2**31 - 1) if self.max_len is None else self.max_len)
+
+
+class RkvPagedCache:
+    """One layer's pool of pages.  The page tables and lengths are the caller's (RkvPagedBatch); `mem` is memory of the
+    caller's for the pool, as it is (uint8, paged_sizes bytes), or None for a cleared pool of its own."""
+
+    def __init__(self, cfg: RkvPagedConfig, device="cuda:0", mem=None):
+        import torch
+        self.cfg, self.lib = cfg, load_library()
+        self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        n = paged_sizes(cfg)
+        if mem is None:
+            mem = torch.zeros(n, dtype=torch.uint8, device=self.device)
+        self.mem = _dev(mem, torch.uint8, "mem")
+        if mem.device != self.device or mem.numel() < n:
+            raise ValueError(f"mem must hold {n} bytes on {self.device}")
+        self.dtype = torch.bfloat16 if cfg.dtype else torch.float16
+        self._c = cfg.to_c()
+
+    def _rows(self, t, heads: int, n_rows: int, what: str):
+        """Pointer and row stride of a tensor [n_rows, heads, head_dim] whose heads are dense."""
+        import torch
+        D = self.cfg.head_dim
+        if not isinstance(t, torch.Tensor) or t.dtype != self.dtype or t.device != self.device:
+            raise TypeError(f"{what} must be a tensor of dtype {self.dtype} on {self.device}")
+        if t.shape != (n_rows, heads, D):
+            raise ValueError(f"{what} must be [{n_rows}, {heads}, {D}]")
+        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != D):
+            raise ValueError(f"{what} must have its heads side by side")
+        return t.data_ptr(), t.stride(0) if n_rows > 1 else heads * D
+
+    def _call(self, batch, name, *args):
+        """One call of the library with the cache's device current."""
+        import torch
+        if batch.device != self.device:
+            raise ValueError(f"the batch must be on {self.device}")
+        cb = batch.to_c(self.cfg)
+        if torch.cuda.current_device() == self.device.index:
+            return self._go(name, cb, *args)
+        with torch.cuda.device(self.device):
+            return self._go(name, cb, *args)
+
+    def _go(self, name, cb, *args):
+        _check(getattr(self.lib, name)(C.byref(self._c), self.mem.data_ptr(), C.byref(cb), *args, _stream()), name)
+
+    def append(self, k, v, batch: RkvPagedBatch):
+        """rkv_paged_append: k, v [n_rows, n_kv_heads, head_dim] of the cache's type (rows may be strided)."""
+        h, n = self.cfg.n_kv_heads, batch.n_rows
+        self._call(batch, "rkv_paged_append", *self._rows(k, h, n, "k"), *self._rows(v, h, n, "v"))
+
+    def read(self, batch: RkvPagedBatch, k=None, v=None):
+        """rkv_paged_read: the rows' keys and values as the cache holds them, into k and v where given."""
+        import torch
+        h, n = self.cfg.n_kv_heads, batch.n_rows
+        shape = (n, h, self.cfg.head_dim)
+        k = torch.empty(shape, dtype=self.dtype, device=self.device) if k is None else k
+        v = torch.empty(shape, dtype=self.dtype, device=self.device) if v is None else v
+        self._call(batch, "rkv_paged_read", *self._rows(k, h, n, "k"), *self._rows(v, h, n, "v"))
+        return k, v
+
+    def attention(self, q, batch: RkvPagedBatch, causal: bool = True, window: int = 0, scale: float = None, out=None, lse=None,
+                  want_lse: bool = False):
+        """rkv_paged_attention: q [n_rows, n_q_heads, head_dim] -> out of the same shape and type (and lse [n_rows, n_q_heads]
+        fp32).  Work space is allocated for each call on its stream, so that calls may overlap."""
+        import torch
+        cfg, n = self.cfg, batch.n_rows
+        qp, qs = self._rows(q, cfg.n_q_heads, n, "q")
+        if out is None:
+            out = torch.empty((n, cfg.n_q_heads, cfg.head_dim), dtype=self.dtype, device=self.device)
+        elif _dev(out, self.dtype, "out").shape != q.shape or out.device != self.device:
+            raise ValueError("out must be a tensor like q")
+        if lse is None and want_lse:
+            lse = torch.empty((n, cfg.n_q_heads), dtype=torch.float32, device=self.device)
+        elif lse is not None and (_dev(lse, torch.float32, "lse").shape != (n, cfg.n_q_heads) or lse.device != self.device):
+            raise ValueError("lse must be [n_rows, n_q_heads]")
+        need, cb = C.c_size_t(0), batch.to_c(cfg)
+        _check(self.lib.rkv_paged_scratch(C.byref(self._c), C.byref(cb), C.byref(need)), "rkv_paged_scratch")
+        scratch = torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None
+        self._call(batch, "rkv_paged_attention", qp, qs, int(causal), window, cfg.head_dim ** -0.5 if scale is None else scale, out.data_ptr(),
+                   _ptr(lse), _ptr(scratch), need.value)
+        return (out, lse) if want_lse else out
