@@ -361,7 +361,7 @@ typedef struct rkv_paged_batch {
   int32_t max_pages;              /* entries of a row of the page table                            */
   int32_t n_rows;                 /* rows of the packed tensors (0: the call does nothing)         */
   int32_t max_new;                /* no sequence has more rows than this, 1..n_rows                */
-  int32_t max_len;                /* nor is one longer than this, 1..max_pages * page_tokens       */
+  int32_t max_len;                /* nor is one longer, 1..max_pages * page_tokens and up to 2^30     */
 } rkv_paged_batch;
 
 /* Bytes of the pool.  RKV_EINVAL if cfg is unsupported. */

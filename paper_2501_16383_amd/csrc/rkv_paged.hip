@@ -184,11 +184,6 @@ __global__ __launch_bounds__(256) void k_paged_read(PagedView v, unsigned short*
       const uint32_t kbyte = sd[0], vbyte = sd[sb << v.page_shift];
       kx = paged_decode8<DT, BITS>(kc, paged_scale(kbyte));
       vx = paged_decode8<DT, BITS>(vc, paged_scale(vbyte));
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        kx[j] = kbyte == 255 ? nan2 : kx[j];
-        vx[j] = vbyte == 255 ? nan2 : vx[j];
-      }
     }
   }
   *(u32x4*)(k + p.row * ks + p.c * 8) = kx;
@@ -242,7 +237,7 @@ static int check_batch(const rkv_paged_config* c, const rkv_paged_batch* b, void
   if (((uintptr_t)b->dev_page_table | (uintptr_t)b->dev_row_start | (uintptr_t)b->dev_lengths) & 3) return RKV_EINVAL;
   if (b->n_seqs < 1 || b->n_seqs > 65536 || b->max_pages < 1) return RKV_EINVAL;
   if (b->max_new < 1 || b->max_new > b->n_rows) return RKV_EINVAL;
-  if (b->max_len < 1 || b->max_len > (int64_t)b->max_pages * c->page_tokens) return RKV_EINVAL;
+  if (b->max_len < 1 || b->max_len > 1 << 30 || b->max_len > (int64_t)b->max_pages * c->page_tokens) return RKV_EINVAL;
   if ((int64_t)b->n_rows * c->n_q_heads > (int64_t)1 << 30) return RKV_EINVAL;   // (the launches' grids)
   if ((uintptr_t)pool & 15) return RKV_EINVAL;
   v->pool = (unsigned char*)pool;

@@ -53,7 +53,7 @@ class RkvPagedBatch:
         n_seqs, max_pages = self.page_table.shape
         return _CPagedBatch(self.page_table.data_ptr(), self.row_start.data_ptr(), self.lengths.data_ptr(), n_seqs, max_pages, self.n_rows,
                             self.n_rows if self.max_new is None else self.max_new,
-                            min(max_pages * cfg.page_tokens, 2**31 - 1) if self.max_len is None else self.max_len)
+                            min(max_pages * cfg.page_tokens, 1 << 30) if self.max_len is None else self.max_len)
 
 
 class RkvPagedCache:

@@ -94,7 +94,7 @@ def check_attention(s, lens, news, got, lse=None, q=None, rows_from=0, **kw):
             l = lse[row:row + m].cpu().double().numpy()
             assert np.array_equal(l == -np.inf, rl == -np.inf)
             fin = rl != -np.inf
-            assert (np.abs(l - rl)[fin] <= (delta[..., 0] + (n + 32) * 2.0**-24 + np.abs(rl) * 2.0**-22)[fin]).all()
+            assert (np.abs(l[fin] - rl[fin]) <= (delta[..., 0] + (n + 32) * 2.0**-24 + np.abs(rl) * 2.0**-22)[fin]).all()
         row += m
 
 
