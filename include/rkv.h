@@ -357,7 +357,7 @@ typedef struct rkv_paged_batch {
   const int32_t* dev_page_table;  /* [n_seqs][max_pages]; entries behind a sequence's last token are not used */
   const int32_t* dev_row_start;   /* [n_seqs + 1], ascending from >= 0 to <= n_rows                */
   const int32_t* dev_lengths;     /* [n_seqs]                                                      */
-  int32_t n_seqs;                 /* 1..65536                                                      */
+  int32_t n_seqs;                 /* 1..65535                                                      */
   int32_t max_pages;              /* entries of a row of the page table                            */
   int32_t n_rows;                 /* rows of the packed tensors (0: the call does nothing)         */
   int32_t max_new;                /* no sequence has more rows than this, 1..n_rows                */

@@ -57,7 +57,8 @@ def stored(x: np.ndarray, bits: int, dtype: str) -> np.ndarray:
 
 def attention(q: np.ndarray, k: np.ndarray, v: np.ndarray, first: int, causal=True, window=0, scale=None):
     """One sequence: q [n, Hq, D] at positions first .., k and v [L, Hkv, D] as stored -> out, lse, and what error bounds
-    need: spread (sum of weight times |v|) and reach (largest sum of |q||k| times the scale over the tokens a row sees)."""
+    need: spread (sum of weight times |v|), reach (largest sum of |q||k| times the scale over the tokens a row sees) and mass
+    (sum of their |v|)."""
     n, Hq, D = q.shape
     L, Hkv = k.shape[:2]
     scale = D**-0.5 if scale is None else scale
@@ -68,7 +69,7 @@ def attention(q: np.ndarray, k: np.ndarray, v: np.ndarray, first: int, causal=Tr
         sees &= t <= p
     if window:
         sees &= t > p - window
-    out, spread = np.zeros((n, Hq, D)), np.zeros((n, Hq, D))
+    out, spread, mass = (np.zeros((n, Hq, D)) for _ in range(3))
     lse, reach = np.full((n, Hq), -np.inf), np.zeros((n, Hq))
     for h in range(Hq):
         g = h // (Hq // Hkv)
@@ -85,5 +86,6 @@ def attention(q: np.ndarray, k: np.ndarray, v: np.ndarray, first: int, causal=Tr
             lse[i, h] = m + np.log(w.sum())
             w /= w.sum()
             out[i, h], spread[i, h] = w @ vv, w @ np.abs(vv)
+            mass[i, h] = np.abs(vv).sum(0)
             reach[i, h] = (np.abs(kk) @ np.abs(q[i, h])).max() * abs(scale)
-    return out, lse, spread, reach
+    return out, lse, spread, reach, mass

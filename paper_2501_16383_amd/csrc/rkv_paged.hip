@@ -235,7 +235,7 @@ static int check_batch(const rkv_paged_config* c, const rkv_paged_batch* b, void
   if (b->n_rows == 0) return RKV_OK;
   if (!b->dev_page_table || !b->dev_row_start || !b->dev_lengths) return RKV_EINVAL;
   if (((uintptr_t)b->dev_page_table | (uintptr_t)b->dev_row_start | (uintptr_t)b->dev_lengths) & 3) return RKV_EINVAL;
-  if (b->n_seqs < 1 || b->n_seqs > 65536 || b->max_pages < 1) return RKV_EINVAL;
+  if (b->n_seqs < 1 || b->n_seqs > 65535 || b->max_pages < 1) return RKV_EINVAL;
   if (b->max_new < 1 || b->max_new > b->n_rows) return RKV_EINVAL;
   if (b->max_len < 1 || b->max_len > 1 << 30 || b->max_len > (int64_t)b->max_pages * c->page_tokens) return RKV_EINVAL;
   if ((int64_t)b->n_rows * c->n_q_heads > (int64_t)1 << 30) return RKV_EINVAL;   // (the launches' grids)

@@ -20,6 +20,12 @@ template <int DT> __device__ __forceinline__ f4 paged_mfma16(u32x4 a, u32x4 b, f
   else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
 }
 
+typedef float f16v __attribute__((ext_vector_type(16)));
+template <int DT> __device__ __forceinline__ f16v paged_mfma32(u32x4 a, u32x4 b, f16v c) {
+  if constexpr (DT) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+}
+
 #define LDS_AS __attribute__((address_space(3)))
 // Four rows of sixteen 16-bit elements, transposed: lane i of a row of 16 gives the address of row i >> 2, elements
 // 4 (i & 3) .., and gets element i of the four rows.
@@ -39,6 +45,16 @@ __device__ __forceinline__ float paged_exp2(float x) { return __builtin_amdgcn_e
 // 2^14, so that one of 2^-28 of it still is a normal number (as a subnormal of 2^-25 it would be off by up to its own size).
 template <int DT> __device__ constexpr float paged_bias() { return DT ? 0.f : 14.f; }
 
+// ... in k_paged_chunk, where weights may pass the largest by 2^8
+template <int DT> __device__ constexpr float paged_chunk_bias() { return DT ? 0.f : 6.f; }
+
+// the value of the lane 32 further
+__device__ __forceinline__ float paged_other(float x, float& mine) {
+  const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+  mine = __uint_as_float(r[0]);
+  return __uint_as_float(r[1]);
+}
+
 // maximum / sum over the four rows of 16 lanes
 __device__ __forceinline__ float paged_max4(float x) {
   u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
@@ -53,18 +69,31 @@ __device__ __forceinline__ float paged_sum4(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Splits of the sequences' tokens: partial results of a work unit (a sequence's columns or a tile of them, and a KV
+// head), as acc [unit][column][split][D] and then (maximum, sum) [unit][column][split]
+struct PagedSplit {
+  int chunk, splits;                  // tokens of a split, most splits of a sequence
+  float* acc;
+  float2* ml;
+};
+
 // What a call asks for beside the batch
 struct PagedAsk {
   const unsigned short* q;
   int64_t qs;
   unsigned short* out;
   float* lse;
-  float* part;                        // partial results of splits: [row][head][split][D + 2]
   float scale2;                       // scale * log2(e)
   int causal, window;
-  int few;                            // rows times rep up to which a sequence goes to k_paged_few (0: no sequence does)
-  int chunk, splits;                  // of k_paged_few: tokens of a split, most splits of a sequence
+  int few;                            // rows times rep up to which a sequence goes to k_paged_few
+  int mixed;                          // sequences with more go to k_paged_chunk (else there are none but bad ones)
+  PagedSplit sp;
 };
+
+// A column's result: out and lse, or the partial result of a split
+template <int DT> __device__ __forceinline__ float paged_lse(float m, float sum) {
+  return sum == 0 ? -INFINITY : (m + __log2f(sum) - paged_bias<DT>()) * 0.69314718055994531f;
+}
 
 // Tokens that the row at position p sees: lo .. hi - 1
 __device__ __forceinline__ int paged_hi_of(const PagedAsk& a, const PagedSeq& s, int p) { return a.causal ? min(max(p + 1, 0), s.len) : s.len; }
@@ -73,8 +102,8 @@ __device__ __forceinline__ int paged_lo_of(const PagedAsk& a, int p) { return a.
 // NaN for every row of a bad sequence that reads this KV head
 template <int D, int DT> __device__ __forceinline__ void paged_bad_rows(const PagedView& v, const PagedAsk& a, int first, int last, int kvh) {
   const int n = (last - first) * v.rep;
-  for (int i = threadIdx.x; i < n * D; i += blockDim.x) {
-    const int c = i / D;
+  for (int64_t i = threadIdx.x; i < (int64_t)n * D; i += blockDim.x) {
+    const int c = (int)(i / D);
     a.out[((int64_t)(first + c / v.rep) * v.Hq + kvh * v.rep + c % v.rep) * D + i % D] = DT ? 0x7fc0 : 0x7e00;
   }
   if (a.lse)
@@ -111,7 +140,7 @@ __global__ __launch_bounds__(256) void k_paged_few(PagedView v, PagedAsk a) {
   const PagedSeq s = paged_seq(v, b);
   const int rows = s.last - s.first, cols = rows * v.rep;
   if (rows == 0) return;
-  if (cols > a.few && v.max_new * v.rep > a.few) return;    // the other kernel's
+  if (cols > a.few && a.mixed) return;                      // the other kernel's
   if (s.bad) {
     if (split == 0) paged_bad_rows<D, DT>(v, a, s.first, s.last, kvh);
     return;
@@ -120,7 +149,7 @@ __global__ __launch_bounds__(256) void k_paged_few(PagedView v, PagedAsk a) {
 
   // tokens that some row sees, and this split's share
   const int all_lo = paged_lo_of(a, s.base), all_hi = paged_hi_of(a, s, s.base + rows - 1);
-  const int from = (all_lo & ~31) + split * a.chunk, to = min(all_hi, from + a.chunk);
+  const int from = (all_lo & ~31) + split * a.sp.chunk, to = min(all_hi, from + a.sp.chunk);
   if (split && from >= all_hi) return;
   // ... that all rows see
   const int full_lo = paged_lo_of(a, s.base + rows - 1), full_hi = paged_hi_of(a, s, s.base);
@@ -286,12 +315,13 @@ __global__ __launch_bounds__(256) void k_paged_few(PagedView v, PagedAsk a) {
           for (int e = 0; e < 4; ++e) pw = (tok >> 4) * 2 + ((tok & 3) >> 1) == e ? p[c][e] : pw;
           pw = __shfl(pw, n + 16 * ((tok >> 2) & 3));
           const float pf = tok & 1 ? paged_hi<DT>(pw) : paged_lo<DT>(pw);
+          const bool sees = t + tok >= lo[c] && t + tok < hi[c];
 #pragma unroll
           for (int k = 0; k < CB; ++k)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const uint32_t bits = vl[tok * PITCH + 16 * k + 4 * g + e];
-              if (paged_odd<DT>(bits) && pf != 0) o[c][k][e] += pf * paged_lo<DT>(bits);
+              if (sees && paged_odd<DT>(bits)) o[c][k][e] += pf * paged_lo<DT>(bits);
             }
         }
       }
@@ -364,104 +394,376 @@ __global__ __launch_bounds__(256) void k_paged_few(PagedView v, PagedAsk a) {
         acc += f * os[(w * 16 + col) * OP + ch];
       }
       const int64_t at = (int64_t)(s.first + cc / v.rep) * v.Hq + kvh * v.rep + cc % v.rep;
-      if (a.splits == 1) {
+      if (a.sp.splits == 1) {
         a.out[at * D + ch] = (unsigned short)paged_pair<DT>(sum == 0 ? 0.f : acc / sum, 0.f);
-        if (a.lse && ch == 0) a.lse[at] = sum == 0 ? -INFINITY : (mm + __log2f(sum) - paged_bias<DT>()) * 0.69314718055994531f;
+        if (a.lse && ch == 0) a.lse[at] = paged_lse<DT>(mm, sum);
       } else {
-        float* part = a.part + (at * a.splits + split) * (D + 2);
-        part[ch] = acc;
-        if (ch == 0) {
-          part[D] = mm;
-          part[D + 1] = sum;
-        }
+        const int64_t u = (((int64_t)b * v.Hkv + kvh) * (16 * NB) + cc) * a.sp.splits + split;
+        a.sp.acc[u * D + ch] = acc;
+        if (ch == 0) a.sp.ml[u] = make_float2(mm, sum);
       }
     }
   }
 }
 
-// The splits of a row and head together: a wave each.
-template <int D, int DT>
-__global__ __launch_bounds__(256) void k_paged_merge(PagedView v, PagedAsk a) {
+// One column's splits together, by a wave: u0 is the first one's index, at the column's place in the output.
+template <int D, int DT> __device__ __forceinline__ void paged_join(const PagedAsk& a, int64_t u0, int n, int64_t at) {
   const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (at >= (int64_t)v.n_rows * v.Hq) return;
-  const int row = __builtin_amdgcn_readfirstlane((int)(at / v.Hq));
-  const int b = paged_owner(v, row);
-  if (b >= v.n_seqs) return;
-  const PagedSeq s = paged_seq(v, b);
-  const int rows = s.last - s.first;
-  if (row < s.first || row >= s.last || s.bad || rows * v.rep > a.few) return;
-  const int all_lo = paged_lo_of(a, s.base), all_hi = paged_hi_of(a, s, s.base + rows - 1);
-  const int n = max(1, (all_hi - (all_lo & ~31) + a.chunk - 1) / a.chunk);
-  const float* part = a.part + at * a.splits * (D + 2);
   float mm = -INFINITY;
-  for (int i = lane; i < n; i += 64) mm = fmaxf(mm, part[(int64_t)i * (D + 2) + D]);
+  for (int i = lane; i < n; i += 64) mm = fmaxf(mm, a.sp.ml[u0 + i].x);
   for (int o = 32; o; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o));
   const float ref = mm == -INFINITY ? 0.f : mm;
   float sum = 0, acc[D / 64] = {};
 #pragma unroll 4
   for (int i = 0; i < n; ++i) {
-    const float* p = part + (int64_t)i * (D + 2);
-    const float f = paged_exp2(p[D] - ref);
-    sum += f * p[D + 1];
+    const float2 ml = a.sp.ml[u0 + i];
+    const float f = paged_exp2(ml.x - ref);
+    sum += f * ml.y;
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) acc[j] += f * p[lane + 64 * j];
+    for (int j = 0; j < D / 64; ++j) acc[j] += f * a.sp.acc[(u0 + i) * D + lane + 64 * j];
   }
 #pragma unroll
   for (int j = 0; j < D / 64; ++j) a.out[at * D + lane + 64 * j] = (unsigned short)paged_pair<DT>(sum == 0 ? 0.f : acc[j] / sum, 0.f);
-  if (a.lse && lane == 0) a.lse[at] = sum == 0 ? -INFINITY : (mm + __log2f(sum) - paged_bias<DT>()) * 0.69314718055994531f;
+  if (a.lse && lane == 0) a.lse[at] = paged_lse<DT>(mm, sum);
 }
 
-// One wave per (row, query head): lanes hold channels, tokens one after the other with the running maximum and
-// sum of the softmax.
-template <int D, int BITS, int DT>
-__global__ __launch_bounds__(64) void k_paged_plain(PagedView v, const unsigned short* __restrict__ q, int64_t qs, int causal, int window,
-                                                    float scale, unsigned short* __restrict__ out, float* __restrict__ lse, int few) {
-  constexpr int N = D / 64;                                      // channels of a lane
-  const int lane = threadIdx.x, row = blockIdx.x / v.Hq, h = blockIdx.x % v.Hq;
-  const int b = paged_owner(v, row);
-  if (b >= v.n_seqs) return;
+template <int D, int DT, int NB>
+__global__ __launch_bounds__(256) void k_paged_merge(PagedView v, PagedAsk a) {
+  const int c = blockIdx.x * 4 + (threadIdx.x >> 6), kvh = blockIdx.y, b = blockIdx.z;
   const PagedSeq s = paged_seq(v, b);
-  if (row < s.first || row >= s.last || (s.last - s.first) * v.rep <= few) return;
-  const int pos = s.base + (row - s.first);
-  const int hi = causal ? min(pos + 1, s.len) : s.len;
-  const int lo = window ? max(0, pos - window + 1) : 0;
-  constexpr int rb = paged_row<D, BITS>(), sb = paged_srow<D, BITS>();
-  auto element = [&](const unsigned char* codes, const unsigned char* scales, int c) {
-    if constexpr (BITS == 16) return paged_lo<DT>(((const unsigned short*)codes)[c]);
-    else {
-      const uint32_t byte = scales[c / 32];
-      if (byte == 255) return __uint_as_float(0x7fc00000);
-      if constexpr (BITS == 8) return paged_lo<DT>(paged_decode2<DT, 8, 0>(codes[c], paged_scale(byte)));
-      else return paged_lo<DT>(paged_decode2<DT, 4, 0>(codes[c / 2] >> (4 * (c & 1)), paged_scale(byte)));
+  const int rows = s.last - s.first, cols = rows * v.rep;
+  if (s.bad || cols > a.few || c >= cols) return;
+  const int lo = paged_lo_of(a, s.base) & ~31, hi = paged_hi_of(a, s, s.base + rows - 1);
+  const int n = max(1, (hi - lo + a.sp.chunk - 1) / a.sp.chunk);
+  paged_join<D, DT>(a, (((int64_t)b * v.Hkv + kvh) * (16 * NB) + c) * a.sp.splits, n,
+                    (int64_t)(s.first + c / v.rep) * v.Hq + kvh * v.rep + c % v.rep);
+}
+
+// ---- many rows: chunks, prompts ----------------------------------------------------------------
+//
+// A workgroup takes 32 NC WAVES columns of one (sequence, KV head), 32 NC a wave, and walks the tokens that they see in
+// tiles of 64.  Tiles are converted to 16 bits as they are staged in LDS, two of them: the next one's bytes come from
+// memory while one is computed, with one barrier a tile.
+#define PAGED_TILE 64
+
+// The tile of columns that a workgroup takes: sequence and first column, or b = n_seqs.  Sequences of more than `few`
+// columns have ceil(columns / COLS) tiles each, numbered through; the last columns, which see most, come first.
+__device__ __forceinline__ int paged_find_tile(const PagedView& v, int few, int per, int tile, int& c0) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int b0 = 0; b0 < v.n_seqs; b0 += 64) {
+    int t = 0;
+    if (b0 + lane < v.n_seqs) {
+      const int f = min(max(v.row_start[b0 + lane], 0), v.n_rows), l = min(max(v.row_start[b0 + lane + 1], f), v.n_rows);
+      const int cols = (l - f) * v.rep;
+      t = cols > few ? (cols + per - 1) / per : 0;
+    }
+    int upto = t;                                           // sum over the lanes up to this one
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(upto, o);
+      if (lane >= o) upto += x;
+    }
+    const uint64_t m = __ballot(before + upto > tile);
+    if (m) {
+      const int i = __builtin_ctzll(m);
+      const int n = __shfl(t, i), first = before + __shfl(upto, i) - n;
+      c0 = (n - 1 - (tile - first)) * per;
+      return b0 + i;
+    }
+    before += __shfl(upto, 63);
+  }
+  c0 = 0;
+  return v.n_seqs;
+}
+
+// 0 in the place of infinities and NaN
+template <int DT> __device__ __forceinline__ uint32_t paged_finite(uint32_t x) {
+  return (paged_odd<DT>(x) ? 0 : x & 0xffffu) | (paged_odd<DT>(x >> 16) ? 0 : x & 0xffff0000u);
+}
+
+template <int D, int BITS, int DT, int WAVES, int NC>
+__global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAsk a) {
+  constexpr int rb = paged_row<D, BITS>(), sb = paged_srow<D, BITS>(), COLS = 32 * NC * WAVES, T = PAGED_TILE, N = WAVES * 64;
+  constexpr int PK = D + 8, PV = D + 32;                    // 16-bit elements between two tokens: reads of 32 keys / of 4 values' parts spread over the banks
+  constexpr int VP = rb / 16, PARTS = 2 * T * VP, R = (PARTS + N - 1) / N;   // 16-byte parts of a row, of a tile (keys, then values), of a thread
+  constexpr int NS = D / 16, CB = D / 32;
+  constexpr float SLACK = 8.f;                              // a maximum may be exceeded by 2^8 before everything is scaled anew
+  __shared__ __align__(16) unsigned short lk[2][T * PK], lv[2][T * PV];
+  __shared__ int odd_tile[2];                               // the last tile in the buffer that held a value which is not finite
+  const int kvh = blockIdx.x % v.Hkv, unit = blockIdx.x / v.Hkv, split = blockIdx.y;
+  int c0;
+  const int b = __builtin_amdgcn_readfirstlane(paged_find_tile(v, a.few, COLS, unit, c0));
+  if (b >= v.n_seqs) return;
+  c0 = __builtin_amdgcn_readfirstlane(c0);
+  const PagedSeq s = paged_seq(v, b);
+  const int rows = s.last - s.first, cols = rows * v.rep;
+  const int r0 = c0 / v.rep, r1 = min(c0 + COLS, cols) - 1;   // first row; last column
+  if (s.bad) {
+    // (rows of this tile's columns; a row whose columns two tiles share is written by both)
+    if (split == 0) paged_bad_rows<D, DT>(v, a, s.first + r0, s.first + r1 / v.rep + 1, kvh);
+    return;
+  }
+  const int all_lo = paged_lo_of(a, s.base + r0), all_hi = paged_hi_of(a, s, s.base + r1 / v.rep);
+  const int from = (all_lo & ~(T - 1)) + split * a.sp.chunk, to = min(all_hi, from + a.sp.chunk);
+  if (split && from >= all_hi) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
+
+  // this wave's columns, and the tokens that some / all of them see
+  const int w0 = c0 + wave * 32 * NC, w1 = min(w0 + 32 * NC, cols) - 1;
+  const bool on = w0 < cols;
+  const int some_lo = on ? paged_lo_of(a, s.base + w0 / v.rep) : 0, some_hi = on ? paged_hi_of(a, s, s.base + w1 / v.rep) : 0;
+  const int full_lo = on ? paged_lo_of(a, s.base + w1 / v.rep) : 0, full_hi = on ? paged_hi_of(a, s, s.base + w0 / v.rep) : 0;
+  u32x4 q[NC][NS];
+  int hi[NC], lo[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int cc = w0 + 32 * c + n, row = cc / v.rep, p = s.base + row;
+    const bool mine = cc < cols;
+    hi[c] = mine ? paged_hi_of(a, s, p) : 0;
+    lo[c] = mine ? paged_lo_of(a, p) : 0;
+#pragma unroll
+    for (int j = 0; j < NS; ++j) {
+      const u32x4 z = {0, 0, 0, 0};
+      q[c][j] = mine ? *(const u32x4*)(a.q + (s.first + row) * a.qs + (kvh * v.rep + cc % v.rep) * D + 16 * j + 8 * h) : z;
+      if (a.scale2 < 0) q[c][j] ^= 0x80008000u;             // (the scale below is its magnitude)
+      if (a.scale2 == 0) q[c][j] = z;
+    }
+  }
+  const float scale2 = a.scale2 == 0 ? 1.f : fabsf(a.scale2);
+  f16v o[NC][CB];
+  float m[NC], l[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    m[c] = -INFINITY;
+    l[c] = 0;
+#pragma unroll
+    for (int k = 0; k < CB; ++k) o[c][k] = f16v{};
+  }
+
+  // staging: part tid + N r of a tile
+  const int mask = (1 << v.page_shift) - 1;
+  const int64_t bb = paged_block<D, BITS>(v.page_shift);
+  const int last_page = (s.len - 1) >> v.page_shift;
+  u32x4 x[R];
+  uint32_t xs[R];
+  int page[R];
+  auto part_of = [&](int r, bool& val, int& tok, int& part) {
+    const int i = tid + N * r;
+    val = i >= T * VP;
+    tok = (i / VP) % T;
+    part = i % VP;
+    return i < PARTS;
+  };
+  auto pages = [&](int t) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      bool val;
+      int tok, part;
+      if (part_of(r, val, tok, part)) page[r] = v.table[(int64_t)b * v.max_pages + min((t + tok) >> v.page_shift, last_page)];
     }
   };
-  float x[N], acc[N], m = -INFINITY, l = 0;
-  for (int j = 0; j < N; ++j) {
-    x[j] = paged_lo<DT>(q[row * qs + h * D + lane + 64 * j]);
-    acc[j] = 0;
+  auto load = [&](int t) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      bool val;
+      int tok, part;
+      if (!part_of(r, val, tok, part)) continue;
+      const bool ok = (unsigned)page[r] < (unsigned)v.n_pages;
+      const unsigned char* blk = v.pool + ((int64_t)(ok ? page[r] : 0) * v.Hkv + kvh) * bb;
+      const int slot = (t + tok) & mask;
+      // values that no row of the tile sees, or of no page, count as zeros; keys of no page as NaN
+      const bool seen = ok && t + tok < all_hi && t + tok >= all_lo;
+      const u32x4 z = {0, 0, 0, 0}, none = {~0u, ~0u, ~0u, ~0u};
+      const u32x4 w = *(const u32x4*)(blk + ((val ? rb : 0) << v.page_shift) + slot * rb + part * 16);
+      x[r] = val ? (seen ? w : z) : (BITS < 16 || ok) ? w : none;
+      if constexpr (BITS < 16) {
+        const uint32_t y = blk[((2 * rb + (val ? sb : 0)) << v.page_shift) + slot * sb + part * (128 / BITS) / 32];
+        xs[r] = val ? (seen ? y : 127) : ok ? y : 255;
+      }
+    }
+  };
+  auto stage = [&](int t, int buf) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      bool val;
+      int tok, part;
+      if (!part_of(r, val, tok, part)) continue;
+      u32x4* d = (u32x4*)((val ? lv[buf] + tok * PV : lk[buf] + tok * PK) + part * (128 / BITS));
+      bool odd = false;
+      if constexpr (BITS == 16) {
+        d[0] = x[r];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd |= paged_odd<DT>(x[r][e]) || paged_odd<DT>(x[r][e] >> 16);
+      } else {
+        odd = xs[r] == 255;
+#pragma unroll
+        for (int e = 0; e < 16 / BITS; ++e) {
+          const u32x2 w = {x[r][BITS == 8 ? 2 * e : e], BITS == 8 ? x[r][2 * e + 1] : 0};
+          d[e] = paged_decode8<DT, BITS>(w, paged_scale(xs[r]));
+        }
+      }
+      if (val && odd) odd_tile[buf] = t;
+    }
+  };
+
+  auto compute = [&](int t, int buf) {
+    const unsigned short *kb = lk[buf], *vb = lv[buf];
+    f16v sc[NC][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) sc[c][i] = f16v{};
+#pragma unroll
+      for (int j = 0; j < NS; ++j) {
+        const u32x4 kk = *(const u32x4*)(kb + (32 * i + n) * PK + 16 * j + 8 * h);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) sc[c][i] = paged_mfma32<DT>(kk, q[c][j], sc[c][i]);
+      }
+    }
+    const bool whole = t >= full_lo && t + T <= full_hi;
+    u32x4 p[NC][4];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      if (!whole) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const int tok = t + 32 * (e >> 4) + 8 * ((e & 15) >> 2) + 4 * h + (e & 3);
+          sc[c][e >> 4][e & 15] = tok >= lo[c] && tok < hi[c] ? sc[c][e >> 4][e & 15] : -INFINITY;
+        }
+      }
+      float top = sc[c][0][0];
+#pragma unroll
+      for (int e = 1; e < 32; ++e) top = fmaxf(top, sc[c][e >> 4][e & 15]);
+      float mine;
+      const float other = paged_other(top, mine);
+      top = fmaxf(mine, other) * scale2;
+      const bool up = top > m[c] + SLACK || (m[c] == -INFINITY && top > m[c]);
+      if (__any(up)) {
+        const float m2 = up ? top : m[c], f = up ? paged_exp2(m[c] - m2) : 1.f;
+        m[c] = m2;
+        l[c] *= f;
+#pragma unroll
+        for (int k = 0; k < CB; ++k) o[c][k] *= f;
+      }
+      const float ref = paged_chunk_bias<DT>() - (m[c] == -INFINITY ? 0.f : m[c]);
+      float sum = 0;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        sc[c][e >> 4][e & 15] = paged_exp2(__builtin_fmaf(sc[c][e >> 4][e & 15], scale2, ref));
+        sum += sc[c][e >> 4][e & 15];
+      }
+      l[c] += sum;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) p[c][e >> 2][e & 3] = paged_pair<DT>(sc[c][e >> 3][2 * (e & 7)], sc[c][e >> 3][2 * (e & 7) + 1]);
+    }
+    // values: lane 16 (2 h + i) + j gives the address of token 4 h + j / 4 (and 8 more), channels 16 i + 4 (j % 4) ..
+    const unsigned short* at = vb + (4 * h + ((lane & 15) >> 2)) * PV + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    const bool fix = !whole && odd_tile[buf] == t;
+    if (fix) {
+      // Values that are not finite, and rows that do not see them: 0 times those is not 0.  Rows that see one take it here; the
+      // products below find a zero in its place.
+#pragma unroll 1
+      for (int tok = 0; tok < T; ++tok) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          uint32_t pw = 0;
+          const int want = (tok >> 5) * 8 + ((tok & 31) >> 3) * 2 + ((tok & 3) >> 1);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) pw = want == e ? p[c][e >> 2][e & 3] : pw;
+          pw = __shfl(pw, n + 32 * ((tok >> 2) & 1));
+          const float pf = tok & 1 ? paged_hi<DT>(pw) : paged_lo<DT>(pw);
+          const bool sees = t + tok >= lo[c] && t + tok < hi[c];
+#pragma unroll
+          for (int k = 0; k < CB; ++k)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const uint32_t bits = vb[tok * PV + 32 * k + 8 * (e >> 2) + 4 * h + (e & 3)];
+              if (sees && paged_odd<DT>(bits)) o[c][k][e] += pf * paged_lo<DT>(bits);
+            }
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int k = 0; k < CB; ++k) {
+        const u32x2 a0 = paged_transposed(at + 16 * j * PV + 32 * k), a1 = paged_transposed(at + (16 * j + 8) * PV + 32 * k);
+        u32x4 vv = {a0[0], a0[1], a1[0], a1[1]};
+        if (fix) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vv[e] = paged_finite<DT>(vv[e]);
+        }
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[c][k] = paged_mfma32<DT>(vv, p[c][j], o[c][k]);
+      }
+  };
+
+  if (tid < 2) odd_tile[tid] = -1;
+  __syncthreads();
+  if (from < to) {
+    pages(from);
+    load(from);
+    if (from + T < to) pages(from + T);
+    stage(from, 0);
   }
-  for (int t = lo; t < hi; ++t) {
-    const int page = paged_page(v, b, t);
-    const unsigned char* blk = v.pool + ((int64_t)max(page, 0) * v.Hkv + h / v.rep) * paged_block<D, BITS>(v.page_shift);
-    const int slot = t & ((1 << v.page_shift) - 1);
-    const unsigned char* sc = blk + ((2 * rb) << v.page_shift) + slot * sb;
-    float d = 0;
-    for (int j = 0; j < N; ++j) d += x[j] * element(blk + slot * rb, sc, lane + 64 * j);
-    for (int o = 32; o; o >>= 1) d += __shfl_xor(d, o);
-    d = page < 0 ? __uint_as_float(0x7fc00000) : d * scale;
-    const float m2 = fmaxf(m, d), ref = m2 == -INFINITY ? 0 : m2;
-    const float a = expf(m - ref), p = expf(d - ref);
-    l = l * a + p;
-    for (int j = 0; j < N; ++j) acc[j] = acc[j] * a + (p > 0 || p != p ? p * element(blk + (rb << v.page_shift) + slot * rb, sc + (sb << v.page_shift), lane + 64 * j) : 0);
-    m = m2;
+  __syncthreads();
+  int buf = 0;
+  for (int t = from; t < to; t += T, buf ^= 1) {
+    const bool more = t + T < to;
+    if (more) {
+      load(t + T);
+      if (t + 2 * T < to) pages(t + 2 * T);
+    }
+    if (t < some_hi && t + T > some_lo) compute(t, buf);
+    if (more) stage(t + T, buf ^ 1);
+    __syncthreads();
   }
-  const float nan = __uint_as_float(0x7fc00000);
-  for (int j = 0; j < N; ++j) {
-    const float o = s.bad ? nan : l == 0 ? 0 : acc[j] / l;
-    out[((int64_t)row * v.Hq + h) * D + lane + 64 * j] = (unsigned short)paged_pair<DT>(o, 0);
+
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int cc = w0 + 32 * c + n;
+    float mine;
+    const float other = paged_other(l[c], mine), sum = mine + other;
+    if (cc >= cols) continue;
+    const int64_t at = (int64_t)(s.first + cc / v.rep) * v.Hq + kvh * v.rep + cc % v.rep;
+    if (a.sp.splits == 1) {
+      const float inv = sum == 0 ? 0.f : 1.f / sum;
+#pragma unroll
+      for (int k = 0; k < CB; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const u32x2 w = {paged_pair<DT>(o[c][k][4 * e] * inv, o[c][k][4 * e + 1] * inv),
+                           paged_pair<DT>(o[c][k][4 * e + 2] * inv, o[c][k][4 * e + 3] * inv)};
+          *(u32x2*)(a.out + at * D + 32 * k + 8 * e + 4 * h) = w;
+        }
+      if (a.lse && h == 0) a.lse[at] = sum == 0 ? -INFINITY : (m[c] + __log2f(sum) - paged_chunk_bias<DT>()) * 0.69314718055994531f;
+    } else {
+      const int64_t u = (((int64_t)unit * v.Hkv + kvh) * COLS + (cc - c0)) * a.sp.splits + split;
+#pragma unroll
+      for (int k = 0; k < CB; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *(f4*)(a.sp.acc + u * D + 32 * k + 8 * e + 4 * h) = f4{o[c][k][4 * e], o[c][k][4 * e + 1], o[c][k][4 * e + 2], o[c][k][4 * e + 3]};
+      // (as k_paged_few's: the merge knows one bias)
+      if (h == 0) a.sp.ml[u] = make_float2(m[c] + (paged_bias<DT>() - paged_chunk_bias<DT>()), sum);
+    }
   }
-  if (lse && lane == 0) lse[(int64_t)row * v.Hq + h] = s.bad ? nan : l == 0 ? -INFINITY : m + logf(l);
+}
+
+template <int D, int DT, int COLS>
+__global__ __launch_bounds__(256) void k_paged_chunk_merge(PagedView v, PagedAsk a) {
+  const int kvh = blockIdx.x % v.Hkv, unit = blockIdx.x / v.Hkv;
+  int c0;
+  const int b = paged_find_tile(v, a.few, COLS, unit, c0);
+  if (b >= v.n_seqs) return;
+  const PagedSeq s = paged_seq(v, b);
+  const int c = blockIdx.y * 4 + (threadIdx.x >> 6), cc = c0 + c, cols = (s.last - s.first) * v.rep;
+  if (s.bad || cc >= cols) return;
+  const int lo = paged_lo_of(a, s.base + c0 / v.rep) & ~(PAGED_TILE - 1);
+  const int hi = paged_hi_of(a, s, s.base + (min(c0 + COLS, cols) - 1) / v.rep);
+  const int n = max(1, (hi - lo + a.sp.chunk - 1) / a.sp.chunk);
+  paged_join<D, DT>(a, (((int64_t)unit * v.Hkv + kvh) * COLS + c) * a.sp.splits, n,
+                    (int64_t)(s.first + cc / v.rep) * v.Hq + kvh * v.rep + cc % v.rep);
 }
 
 // ---- host side ---------------------------------------------------------------------------------
@@ -469,38 +771,81 @@ __global__ __launch_bounds__(64) void k_paged_plain(PagedView v, const unsigned 
 #define RKV_PAGED_CUS 256             // compute units that a launch should fill
 #define RKV_PAGED_FEW 32              // columns (rows times rep) of a sequence that k_paged_few takes
 #define RKV_PAGED_SPLITS 256          // most splits of a sequence
+#define RKV_PAGED_COLS 256            // columns of a workgroup of k_paged_chunk
 
-// Splits of k_paged_few: as many tokens each (a multiple of 128: 32 for each wave) as let the workgroups of sequences
-// of max_len tokens fill the device twice.
-static void few_splits(const PagedView& v, int window, int* chunk, int* splits) {
-  int64_t span = v.max_len;                                 // (the rows are a sequence's last tokens, with or without `causal`)
-  if (window && span > (int64_t)window + v.max_new + 31) span = (int64_t)window + v.max_new + 31;
-  const int64_t pairs = (int64_t)v.n_seqs * v.Hkv, want = (2 * RKV_PAGED_CUS + pairs - 1) / pairs;
-  int64_t c = ((span + want - 1) / want + 127) / 128 * 128;
-  const int64_t least = ((span + RKV_PAGED_SPLITS - 1) / RKV_PAGED_SPLITS + 127) / 128 * 128;
-  if (c < least) c = least;
-  *chunk = (int)c;
-  *splits = (int)((span + c - 1) / c);
+// Splits of sequences of max_len tokens whose work units (`units` of them) should become `want`: a multiple of `step` tokens each.
+static void paged_cut(const PagedView& v, int window, int tile, int64_t units, int64_t want, int step, int rows, PagedSplit* sp) {
+  int64_t span = v.max_len;
+  if (window && span > (int64_t)window + rows + tile - 1) span = (int64_t)window + rows + tile - 1;
+  int64_t n = (want + units - 1) / units;
+  if (n > RKV_PAGED_SPLITS) n = RKV_PAGED_SPLITS;
+  const int64_t c = ((span + n - 1) / n + step - 1) / step * step;
+  sp->chunk = (int)c;
+  sp->splits = (int)((span + c - 1) / c);
+}
+// Bytes of partial results, for any window (a shorter span may be cut into more splits than a longer one, but never into
+// more than are wanted)
+static size_t paged_cut_bytes(const PagedView& v, int64_t units, int64_t want, int step, int cols, int D) {
+  int64_t n = (want + units - 1) / units, cut = ((int64_t)v.max_len + step - 1) / step;
+  if (n > RKV_PAGED_SPLITS) n = RKV_PAGED_SPLITS;
+  if (n > cut) n = cut;
+  return n > 1 ? (size_t)units * cols * n * (D + 2) * 4 : 0;
 }
 
-// (for any window: a shorter span may be cut into more splits, but not into more than are wanted)
+// k_paged_few: a unit is a (sequence, KV head); two workgroups for each compute unit, splits of at least 128 tokens (32 for
+// each wave)
+static int64_t few_units(const PagedView& v) { return (int64_t)v.n_seqs * v.Hkv; }
+static int few_cols(const PagedView& v) { return (int64_t)v.max_new * v.rep <= 16 ? 16 : 32; }
+#define FEW_WANT (2 * RKV_PAGED_CUS)
+#define FEW_STEP 128
+// k_paged_chunk: a unit is a tile of columns and a KV head; a workgroup for each compute unit, splits of at least 512 tokens
+static int64_t chunk_units(const PagedView& v) {
+  // every sequence may have a tile that is not full
+  const int64_t cols = (int64_t)v.n_rows * v.rep, seqs = v.n_seqs < cols / RKV_PAGED_FEW ? v.n_seqs : cols / RKV_PAGED_FEW;
+  return (cols / RKV_PAGED_COLS + seqs) * v.Hkv;
+}
+#define CHUNK_WANT RKV_PAGED_CUS
+#define CHUNK_STEP 512
+static bool has_few(const PagedView& v) { return v.n_seqs > 1 || (int64_t)v.max_new * v.rep <= RKV_PAGED_FEW; }
+static bool has_chunk(const PagedView& v) { return (int64_t)v.max_new * v.rep > RKV_PAGED_FEW; }
+
+// work space: k_paged_few's partial results, then k_paged_chunk's
+static size_t few_bytes(const PagedView& v, int D) {
+  const size_t n = has_few(v) ? paged_cut_bytes(v, few_units(v), FEW_WANT, FEW_STEP, few_cols(v), D) : 0;
+  return (n + 255) & ~(size_t)255;
+}
 size_t rkv_paged_attention_scratch(const PagedView& v, int D) {
-  const int64_t pairs = (int64_t)v.n_seqs * v.Hkv, want = (2 * RKV_PAGED_CUS + pairs - 1) / pairs, cut = ((int64_t)v.max_len + 127) / 128;
-  int64_t splits = want < cut ? want : cut;
-  if (splits > RKV_PAGED_SPLITS) splits = RKV_PAGED_SPLITS;
-  return splits > 1 ? (size_t)v.n_rows * v.Hq * splits * (D + 2) * 4 : 0;
+  return few_bytes(v, D) + (has_chunk(v) ? paged_cut_bytes(v, chunk_units(v), CHUNK_WANT, CHUNK_STEP, RKV_PAGED_COLS, D) : 0);
+}
+
+template <int D, int BITS, int DT, int NB>
+static void launch_few(const PagedView& v, PagedAsk a, void* scratch, hipStream_t s) {
+  paged_cut(v, a.window, 32, few_units(v), FEW_WANT, FEW_STEP, RKV_PAGED_FEW, &a.sp);
+  a.sp.acc = (float*)scratch;
+  a.sp.ml = (float2*)(a.sp.acc + few_units(v) * (16 * NB) * a.sp.splits * D);
+  k_paged_few<D, BITS, DT, NB><<<dim3(a.sp.splits, v.Hkv, v.n_seqs), 256, 0, s>>>(v, a);
+  if (a.sp.splits > 1) k_paged_merge<D, DT, NB><<<dim3(4 * NB, v.Hkv, v.n_seqs), 256, 0, s>>>(v, a);
 }
 
 template <int D, int BITS, int DT>
-static void launch(const PagedView& v, PagedAsk a, hipStream_t s) {
-  few_splits(v, a.window, &a.chunk, &a.splits);
+static void launch(const PagedView& v, PagedAsk a, void* scratch, hipStream_t s) {
   a.few = RKV_PAGED_FEW;
-  const dim3 grid(a.splits, v.Hkv, v.n_seqs);
-  if (v.max_new * v.rep <= 16) k_paged_few<D, BITS, DT, 1><<<grid, 256, 0, s>>>(v, a);
-  else k_paged_few<D, BITS, DT, 2><<<grid, 256, 0, s>>>(v, a);
-  if (v.max_new * v.rep > RKV_PAGED_FEW)
-    k_paged_plain<D, BITS, DT><<<dim3(v.n_rows * v.Hq), 64, 0, s>>>(v, a.q, a.qs, a.causal, a.window, a.scale2 / 1.4426950408889634f, a.out, a.lse, a.few);
-  if (a.splits > 1) k_paged_merge<D, DT><<<dim3((unsigned)(((int64_t)v.n_rows * v.Hq + 3) / 4)), 256, 0, s>>>(v, a);
+  a.mixed = has_chunk(v);
+  if (has_few(v)) {
+    if (few_cols(v) == 16) launch_few<D, BITS, DT, 1>(v, a, scratch, s);
+    else launch_few<D, BITS, DT, 2>(v, a, scratch, s);
+  }
+  if (a.mixed) {
+    if (!has_few(v)) a.few = 0;
+    const int64_t units = chunk_units(v);
+    // (rows of a unit; without `causal` its first row sees all behind it)
+    const int rows = a.causal && v.max_new > RKV_PAGED_COLS ? RKV_PAGED_COLS : v.max_new;
+    paged_cut(v, a.window, PAGED_TILE, units, CHUNK_WANT, CHUNK_STEP, rows, &a.sp);
+    a.sp.acc = (float*)((char*)scratch + few_bytes(v, D));
+    a.sp.ml = (float2*)(a.sp.acc + units * RKV_PAGED_COLS * a.sp.splits * D);
+    k_paged_chunk<D, BITS, DT, 8, 1><<<dim3((unsigned)units, a.sp.splits), 512, 0, s>>>(v, a);
+    if (a.sp.splits > 1) k_paged_chunk_merge<D, DT, RKV_PAGED_COLS><<<dim3((unsigned)units, RKV_PAGED_COLS / 4), 256, 0, s>>>(v, a);
+  }
 }
 
 int rkv_launch_paged_attention(const PagedView& v, int D, int bits, int dtype, const void* q, int64_t qs, int causal, int window, float scale,
@@ -510,11 +855,10 @@ int rkv_launch_paged_attention(const PagedView& v, int D, int bits, int dtype, c
   a.qs = qs;
   a.out = (unsigned short*)out;
   a.lse = lse;
-  a.part = (float*)scratch;
   a.scale2 = (float)((double)scale * 1.4426950408889634);
   a.causal = causal;
   a.window = window < 1 << 30 ? window : 1 << 30;            // (no sequence is longer)
-#define GO(D_, B_) (dtype ? launch<D_, B_, 1>(v, a, s) : launch<D_, B_, 0>(v, a, s))
+#define GO(D_, B_) (dtype ? launch<D_, B_, 1>(v, a, scratch, s) : launch<D_, B_, 0>(v, a, scratch, s))
   if (D == 64) { if (bits == 16) GO(64, 16); else if (bits == 8) GO(64, 8); else GO(64, 4); }
   else { if (bits == 16) GO(128, 16); else if (bits == 8) GO(128, 8); else GO(128, 4); }
 #undef GO

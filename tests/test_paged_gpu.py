@@ -6,7 +6,9 @@ a score is off by at most delta = reach * (D + 8) * 2^-24 (reach: the sum of |q|
 roundings of the scale, the maximum's subtraction and the exponential's argument), which moves every weight by a factor of
 at most 1 + 2 delta; a weight is rounded to the type before it multiplies a value (u) and the exponential and the division
 are off by a few 2^-23; n products are summed in fp32 (n * 2^-24).  All of these count on spread = sum of weight * |v|.  The output
-is rounded once more (u * |out|, or half a step of the type's smallest numbers).
+is rounded once more (u * |out|, or half a step of the type's smallest numbers).  A weight too small for u is rounded by half
+a step of the type's subnormal numbers: fp16 weights are held times at least 2^6, the largest being 2^6 or more, so that this is
+at most 2^-25 / 2^6 = 2^-31 of the largest weight and of their sum, and counts on mass = sum of |v| (bf16: 2^-134, nothing).
 """
 import numpy as np
 import pytest
@@ -81,12 +83,13 @@ class Setup:
 def check_attention(s, lens, news, got, lse=None, q=None, rows_from=0, **kw):
     u = torch.finfo(TYPES[s.dtype]).eps / 2
     tiny = 2.0 ** (-25 if s.dtype == "fp16" else -134)
+    least = 2.0**-31 if s.dtype == "fp16" else 0
     row = rows_from
     got, q = got.cpu().double().numpy(), q.cpu().double().numpy()
     for b, (n, m) in enumerate(zip(lens, news)):
-        ref, rl, spread, reach = O.attention(q[row:row + m], s.held(s.k, b, n), s.held(s.v, b, n), n - m, **kw)
+        ref, rl, spread, reach, mass = O.attention(q[row:row + m], s.held(s.k, b, n), s.held(s.v, b, n), n - m, **kw)
         delta = (reach * (s.D + 8) * 2.0**-24)[..., None]
-        tol = spread * (u + 2 * delta + (n + 16) * 2.0**-24) * 1.001 + u * np.abs(ref) + tiny
+        tol = spread * (u + 2 * delta + (n + 16) * 2.0**-24) * 1.001 + u * np.abs(ref) + tiny + mass * least
         err = np.abs(got[row:row + m] - ref)
         assert np.isfinite(got[row:row + m]).all(), b
         assert (err <= tol).all(), (b, n, m, (err / np.maximum(tol, 1e-300)).max())
