@@ -7,6 +7,8 @@
 // the four (eight) weights a lane gets from the first product are, in their order, an operand of the second.
 // (Which token is which index of the sum is free as long as both operands agree.)  Weights are powers of two of
 // scores in fp32; the sum of weights is taken in fp32 from unrounded weights.
+#include <type_traits>
+
 #include "rkv_mfma_ops.h"
 #include "rkv_paged.h"
 
@@ -27,6 +29,7 @@ template <int DT> __device__ __forceinline__ f16v paged_mfma32(u32x4 a, u32x4 b,
 }
 
 #define LDS_AS __attribute__((address_space(3)))
+#define PAGED_CONST __attribute__((address_space(4)))      // not written while a kernel runs: scalar loads
 // Four rows of sixteen 16-bit elements, transposed: lane i of a row of 16 gives the address of row i >> 2, elements
 // 4 (i & 3) .., and gets element i of the four rows.
 __device__ __forceinline__ u32x2 paged_transposed(const unsigned short* p) {
@@ -508,11 +511,10 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
   if (split && from >= all_hi) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
 
-  // this wave's columns, and the tokens that some / all of them see
+  // this wave's columns, and the tokens that some of them see
   const int w0 = c0 + wave * 32 * NC, w1 = min(w0 + 32 * NC, cols) - 1;
   const bool on = w0 < cols;
   const int some_lo = on ? paged_lo_of(a, s.base + w0 / v.rep) : 0, some_hi = on ? paged_hi_of(a, s, s.base + w1 / v.rep) : 0;
-  const int full_lo = on ? paged_lo_of(a, s.base + w1 / v.rep) : 0, full_hi = on ? paged_hi_of(a, s, s.base + w0 / v.rep) : 0;
   u32x4 q[NC][NS];
   int hi[NC], lo[NC];
 #pragma unroll
@@ -540,73 +542,99 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
     for (int k = 0; k < CB; ++k) o[c][k] = f16v{};
   }
 
-  // staging: part tid + N r of a tile
+  // Staging: a wave's load r takes 64 neighbouring parts, which lie in one page (in the pages of two sixteens of
+  // tokens where a row is but two parts) and one after the other in memory: scalar addresses plus 16 bytes a lane.
+  constexpr int TL = 64 / VP;                               // tokens of a wave's load
   const int mask = (1 << v.page_shift) - 1;
   const int64_t bb = paged_block<D, BITS>(v.page_shift);
   const int last_page = (s.len - 1) >> v.page_shift;
+  const PAGED_CONST int* table = (const PAGED_CONST int*)(v.table + (int64_t)b * v.max_pages);
+  const int ltok = lane / VP, lpart = lane % VP;
   u32x4 x[R];
   uint32_t xs[R];
-  int page[R];
-  auto part_of = [&](int r, bool& val, int& tok, int& part) {
-    const int i = tid + N * r;
-    val = i >= T * VP;
-    tok = (i / VP) % T;
-    part = i % VP;
-    return i < PARTS;
-  };
+  int page[R][TL > 16 ? 2 : 1];
+  // load r of this wave: keys or values, and its first token
+  auto first_part = [&](int r) { return 64 * (wave + WAVES * r); };
+  auto has = [&](int r) { return N * r + N <= PARTS || first_part(r) < PARTS; };
+  auto is_val = [&](int r) { return N * r >= T * VP || (N * r + N > T * VP && first_part(r) >= T * VP); };
+  auto tok_of = [&](int r) { return first_part(r) / VP % T; };
   auto pages = [&](int t) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      bool val;
-      int tok, part;
-      if (part_of(r, val, tok, part)) page[r] = v.table[(int64_t)b * v.max_pages + min((t + tok) >> v.page_shift, last_page)];
-    }
-  };
-  auto load = [&](int t) {
+    for (int r = 0; r < R; ++r)
+      if (has(r)) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      bool val;
-      int tok, part;
-      if (!part_of(r, val, tok, part)) continue;
-      const bool ok = (unsigned)page[r] < (unsigned)v.n_pages;
-      const unsigned char* blk = v.pool + ((int64_t)(ok ? page[r] : 0) * v.Hkv + kvh) * bb;
-      const int slot = (t + tok) & mask;
-      // values that no row of the tile sees, or of no page, count as zeros; keys of no page as NaN
-      const bool seen = ok && t + tok < all_hi && t + tok >= all_lo;
-      const u32x4 z = {0, 0, 0, 0}, none = {~0u, ~0u, ~0u, ~0u};
-      const u32x4 w = *(const u32x4*)(blk + ((val ? rb : 0) << v.page_shift) + slot * rb + part * 16);
-      x[r] = val ? (seen ? w : z) : (BITS < 16 || ok) ? w : none;
-      if constexpr (BITS < 16) {
-        const uint32_t y = blk[((2 * rb + (val ? sb : 0)) << v.page_shift) + slot * sb + part * (128 / BITS) / 32];
-        xs[r] = val ? (seen ? y : 127) : ok ? y : 255;
+        for (int i = 0; i < (TL > 16 ? 2 : 1); ++i) page[r][i] = table[min((t + tok_of(r) + 16 * i) >> v.page_shift, last_page)];
       }
-    }
   };
-  auto stage = [&](int t, int buf) {
+  int page_was[R][TL > 16 ? 2 : 1];                         // of the tile in x
+  bool gone = false;                                        // a page of it is none of the pool's
+  auto load = [&](int t) {
+    gone = false;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      bool val;
-      int tok, part;
-      if (!part_of(r, val, tok, part)) continue;
-      u32x4* d = (u32x4*)((val ? lv[buf] + tok * PV : lk[buf] + tok * PK) + part * (128 / BITS));
-      bool odd = false;
-      if constexpr (BITS == 16) {
-        d[0] = x[r];
+    for (int r = 0; r < R; ++r)
+      if (has(r)) {
+        const bool val = is_val(r);
+        const unsigned char* at[TL > 16 ? 2 : 1];           // first code, first scale
+        const unsigned char* sat[TL > 16 ? 2 : 1];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) odd |= paged_odd<DT>(x[r][e]) || paged_odd<DT>(x[r][e] >> 16);
-      } else {
-        odd = xs[r] == 255;
-#pragma unroll
-        for (int e = 0; e < 16 / BITS; ++e) {
-          const u32x2 w = {x[r][BITS == 8 ? 2 * e : e], BITS == 8 ? x[r][2 * e + 1] : 0};
-          d[e] = paged_decode8<DT, BITS>(w, paged_scale(xs[r]));
+        for (int i = 0; i < (TL > 16 ? 2 : 1); ++i) {
+          page_was[r][i] = page[r][i];
+          const bool ok = (unsigned)page[r][i] < (unsigned)v.n_pages;
+          gone |= !ok;
+          const unsigned char* blk = v.pool + ((int64_t)(ok ? page[r][i] : 0) * v.Hkv + kvh) * bb;
+          const int slot = (t + tok_of(r) + 16 * i) & mask;
+          at[i] = blk + ((val ? rb : 0) << v.page_shift) + slot * rb;
+          sat[i] = blk + ((2 * rb + (val ? sb : 0)) << v.page_shift) + slot * sb;
+        }
+        if constexpr (TL > 16) {
+          x[r] = *(const u32x4*)((lane < 32 ? at[0] : at[1]) + (lane & 31) * 16);
+          xs[r] = ((lane < 32 ? sat[0] : sat[1]) + (ltok & 15) * sb)[lpart * (128 / BITS) / 32];
+        } else {
+          x[r] = *(const u32x4*)(at[0] + lane * 16);
+          if constexpr (BITS < 16) xs[r] = (sat[0] + ltok * sb)[lpart * (128 / BITS) / 32];
         }
       }
-      if (val && odd) odd_tile[buf] = t;
-    }
+  };
+  // rows that all columns of the workgroup see whole
+  const int wg_lo = paged_lo_of(a, s.base + r1 / v.rep), wg_hi = paged_hi_of(a, s, s.base + r0);
+  auto stage = [&](int t, int buf) {
+    const bool plain = t >= wg_lo && t + T <= wg_hi && !gone;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (has(r)) {
+        const bool val = is_val(r);
+        const int tok = tok_of(r) + ltok;
+        if (__builtin_expect(!plain, 0)) {
+          // values that no row of the tile sees, or of no page, count as zeros; keys of no page as NaN
+          const int pg = TL > 16 && lane >= 32 ? page_was[r][TL > 16 ? 1 : 0] : page_was[r][0];
+          const bool ok = (unsigned)pg < (unsigned)v.n_pages, seen = ok && t + tok < all_hi && t + tok >= all_lo;
+          const u32x4 z = {0, 0, 0, 0}, none = {~0u, ~0u, ~0u, ~0u};
+          if (val) x[r] = seen ? x[r] : z;
+          else if (BITS == 16) x[r] = ok ? x[r] : none;
+          bool odd = false;
+          if constexpr (BITS < 16) {
+            xs[r] = val ? (seen ? xs[r] : 127) : ok ? xs[r] : 255;
+            odd = xs[r] == 255;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd |= paged_odd<DT>(x[r][e]) || paged_odd<DT>(x[r][e] >> 16);
+          }
+          if (val && odd) odd_tile[buf] = t;
+        }
+        u32x4* d = (u32x4*)((val ? lv[buf] + tok * PV : lk[buf] + tok * PK) + lpart * (128 / BITS));
+        if constexpr (BITS == 16) d[0] = x[r];
+        else {
+#pragma unroll
+          for (int e = 0; e < 16 / BITS; ++e) {
+            const u32x2 w = {x[r][BITS == 8 ? 2 * e : e], BITS == 8 ? x[r][2 * e + 1] : 0};
+            d[e] = paged_decode8<DT, BITS>(w, paged_scale(xs[r]));
+          }
+        }
+      }
   };
 
-  auto compute = [&](int t, int buf) {
+  auto compute = [&](auto masked, int t, int buf) {         // masked: some column does not see some token
+    constexpr bool MASKED = decltype(masked)::value;
     const unsigned short *kb = lk[buf], *vb = lv[buf];
     f16v sc[NC][2];
 #pragma unroll
@@ -620,11 +648,10 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
         for (int c = 0; c < NC; ++c) sc[c][i] = paged_mfma32<DT>(kk, q[c][j], sc[c][i]);
       }
     }
-    const bool whole = t >= full_lo && t + T <= full_hi;
     u32x4 p[NC][4];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      if (!whole) {
+      if constexpr (MASKED) {
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
           const int tok = t + 32 * (e >> 4) + 8 * ((e & 15) >> 2) + 4 * h + (e & 3);
@@ -658,8 +685,8 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
     }
     // values: lane 16 (2 h + i) + j gives the address of token 4 h + j / 4 (and 8 more), channels 16 i + 4 (j % 4) ..
     const unsigned short* at = vb + (4 * h + ((lane & 15) >> 2)) * PV + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-    const bool fix = !whole && odd_tile[buf] == t;
-    if (fix) {
+    const bool fix = MASKED && odd_tile[buf] == t;
+    if (MASKED && fix) {
       // Values that are not finite, and rows that do not see them: 0 times those is not 0.  Rows that see one take it here; the
       // products below find a zero in its place.
 #pragma unroll 1
@@ -683,41 +710,57 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
         }
       }
     }
+    auto products = [&](auto finite) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int k = 0; k < CB; ++k) {
-        const u32x2 a0 = paged_transposed(at + 16 * j * PV + 32 * k), a1 = paged_transposed(at + (16 * j + 8) * PV + 32 * k);
-        u32x4 vv = {a0[0], a0[1], a1[0], a1[1]};
-        if (fix) {
+        for (int k = 0; k < CB; ++k) {
+          const u32x2 a0 = paged_transposed(at + 16 * j * PV + 32 * k), a1 = paged_transposed(at + (16 * j + 8) * PV + 32 * k);
+          u32x4 vv = {a0[0], a0[1], a1[0], a1[1]};
+          if constexpr (decltype(finite)::value) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) vv[e] = paged_finite<DT>(vv[e]);
+            for (int e = 0; e < 4; ++e) vv[e] = paged_finite<DT>(vv[e]);
+          }
+#pragma unroll
+          for (int c = 0; c < NC; ++c) o[c][k] = paged_mfma32<DT>(vv, p[c][j], o[c][k]);
         }
-#pragma unroll
-        for (int c = 0; c < NC; ++c) o[c][k] = paged_mfma32<DT>(vv, p[c][j], o[c][k]);
-      }
+    };
+    if constexpr (MASKED) {
+      if (fix) products(std::true_type{});
+      else products(std::false_type{});
+    } else products(std::false_type{});
   };
 
+  // The tiles' order: those that not all columns see whole first (in front of a window's end, then the last tokens'), in a loop
+  // of their own, so that the loop over the others holds nothing else.
+  const int whole_from = max(from, (wg_lo + T - 1) & ~(T - 1)), whole_to = min(to, wg_hi & ~(T - 1));
+  const int tiles = from < to ? (to - from + T - 1) / T : 0, whole = max(0, (whole_to - whole_from) / T), partial = tiles - whole;
+  const int front = whole ? (whole_from - from) / T : tiles;
+  auto tile_at = [&](int i) { return i < front ? from + i * T : i < partial ? whole_to + (i - front) * T : whole_from + (i - partial) * T; };
   if (tid < 2) odd_tile[tid] = -1;
   __syncthreads();
-  if (from < to) {
-    pages(from);
-    load(from);
-    if (from + T < to) pages(from + T);
-    stage(from, 0);
+  if (tiles > 0) {
+    pages(tile_at(0));
+    load(tile_at(0));
+    if (tiles > 1) pages(tile_at(1));
+    stage(tile_at(0), 0);
   }
   __syncthreads();
-  int buf = 0;
-  for (int t = from; t < to; t += T, buf ^= 1) {
-    const bool more = t + T < to;
-    if (more) {
-      load(t + T);
-      if (t + 2 * T < to) pages(t + 2 * T);
+  int i = 0;
+  auto walk = [&](auto masked, int end) {
+    for (; i < end; ++i) {
+      const int t = tile_at(i), buf = i & 1;
+      if (i + 1 < tiles) {
+        load(tile_at(i + 1));
+        if (i + 2 < tiles) pages(tile_at(i + 2));
+      }
+      if (!decltype(masked)::value || (t < some_hi && t + T > some_lo)) compute(masked, t, buf);
+      if (i + 1 < tiles) stage(tile_at(i + 1), buf ^ 1);
+      __syncthreads();
     }
-    if (t < some_hi && t + T > some_lo) compute(t, buf);
-    if (more) stage(t + T, buf ^ 1);
-    __syncthreads();
-  }
+  };
+  walk(std::true_type{}, partial);
+  walk(std::false_type{}, tiles);
 
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
