@@ -29,6 +29,7 @@ template <int DT> __device__ __forceinline__ f16v paged_mfma32(u32x4 a, u32x4 b,
 }
 
 #define LDS_AS __attribute__((address_space(3)))
+#define PAGED_INLINE __attribute__((always_inline))
 #define PAGED_CONST __attribute__((address_space(4)))      // not written while a kernel runs: scalar loads
 // Four rows of sixteen 16-bit elements, transposed: lane i of a row of 16 gives the address of row i >> 2, elements
 // 4 (i & 3) .., and gets element i of the four rows.
@@ -188,11 +189,11 @@ __global__ __launch_bounds__(256) void k_paged_few(PagedView v, PagedAsk a) {
   const int64_t bb = paged_block<D, BITS>(v.page_shift);
   const int last_page = (s.len - 1) >> v.page_shift;        // (len > 0 where there is a tile at all)
 
-  auto pages = [&](int t, int* p) {
+  auto pages = [&](int t, int* p) PAGED_INLINE {
 #pragma unroll
     for (int i = 0; i < 2; ++i) p[i] = v.table[(int64_t)b * v.max_pages + min((t + 16 * i) >> v.page_shift, last_page)];
   };
-  auto load = [&](int t, const int* p, Tile& x) {
+  auto load = [&](int t, const int* p, Tile& x) PAGED_INLINE {
     const unsigned char* blk[2];
     bool ok[2];
 #pragma unroll
@@ -230,7 +231,7 @@ __global__ __launch_bounds__(256) void k_paged_few(PagedView v, PagedAsk a) {
       if constexpr (BITS < 16) x.vs[r] = seen ? base[((2 * rb + sb) << v.page_shift) + slot * sb + part * (128 / BITS) / 32] : 127;
     }
   };
-  auto compute = [&](int t, const Tile& x) {
+  auto compute = [&](int t, const Tile& x) PAGED_INLINE {
     // values to LDS as 16-bit rows
     bool odd = false;                                       // holds infinities or NaN
 #pragma unroll
@@ -444,7 +445,7 @@ __global__ __launch_bounds__(256) void k_paged_merge(PagedView v, PagedAsk a) {
 
 // ---- many rows: chunks, prompts ----------------------------------------------------------------
 //
-// A workgroup takes 32 NC WAVES columns of one (sequence, KV head), 32 NC a wave, and walks the tokens that they see in
+// A workgroup takes 32 WAVES columns of one (sequence, KV head), 32 a wave, and walks the tokens that they see in
 // tiles of 64.  Tiles are converted to 16 bits as they are staged in LDS, two of them: the next one's bytes come from
 // memory while one is computed, with one barrier a tile.
 #define PAGED_TILE 64
@@ -484,15 +485,15 @@ template <int DT> __device__ __forceinline__ uint32_t paged_finite(uint32_t x) {
   return (paged_odd<DT>(x) ? 0 : x & 0xffffu) | (paged_odd<DT>(x >> 16) ? 0 : x & 0xffff0000u);
 }
 
-template <int D, int BITS, int DT, int WAVES, int NC>
+template <int D, int BITS, int DT, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAsk a) {
-  constexpr int rb = paged_row<D, BITS>(), sb = paged_srow<D, BITS>(), COLS = 32 * NC * WAVES, T = PAGED_TILE, N = WAVES * 64;
+  constexpr int rb = paged_row<D, BITS>(), sb = paged_srow<D, BITS>(), COLS = 32 * WAVES, T = PAGED_TILE, N = WAVES * 64;
   constexpr int PK = D + 8, PV = D + 32;                    // 16-bit elements between two tokens: reads of 32 keys / of 4 values' parts spread over the banks
-  constexpr int VP = rb / 16, PARTS = 2 * T * VP, R = (PARTS + N - 1) / N;   // 16-byte parts of a row, of a tile (keys, then values), of a thread
+  constexpr int VP = rb / 16;                               // 16-byte parts of a row
   constexpr int NS = D / 16, CB = D / 32;
   constexpr float SLACK = 8.f;                              // a maximum may be exceeded by 2^8 before everything is scaled anew
-  __shared__ __align__(16) unsigned short lk[2][T * PK], lv[2][T * PV];
-  __shared__ int odd_tile[2];                               // the last tile in the buffer that held a value which is not finite
+  __shared__ __align__(16) unsigned short lk[3][T * PK], lv[4][T * PV];
+  __shared__ int odd_tile[4];                               // the last tile in the buffer that held a value which is not finite
   const int kvh = blockIdx.x % v.Hkv, unit = blockIdx.x / v.Hkv, split = blockIdx.y;
   int c0;
   const int b = __builtin_amdgcn_readfirstlane(paged_find_tile(v, a.few, COLS, unit, c0));
@@ -511,224 +512,204 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
   if (split && from >= all_hi) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
 
-  // this wave's columns, and the tokens that some of them see
-  const int w0 = c0 + wave * 32 * NC, w1 = min(w0 + 32 * NC, cols) - 1;
-  const bool on = w0 < cols;
-  const int some_lo = on ? paged_lo_of(a, s.base + w0 / v.rep) : 0, some_hi = on ? paged_hi_of(a, s, s.base + w1 / v.rep) : 0;
-  u32x4 q[NC][NS];
-  int hi[NC], lo[NC];
+  // this lane's column, and the tokens it sees
+  const int cc = c0 + wave * 32 + n, pos = s.base + cc / v.rep;
+  const bool mine = cc < cols;
+  const int hi = mine ? paged_hi_of(a, s, pos) : 0, lo = mine ? paged_lo_of(a, pos) : 0;
+  const int64_t at = (int64_t)(s.first + cc / v.rep) * v.Hq + kvh * v.rep + cc % v.rep;
+  u32x4 q[NS];
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int cc = w0 + 32 * c + n, row = cc / v.rep, p = s.base + row;
-    const bool mine = cc < cols;
-    hi[c] = mine ? paged_hi_of(a, s, p) : 0;
-    lo[c] = mine ? paged_lo_of(a, p) : 0;
-#pragma unroll
-    for (int j = 0; j < NS; ++j) {
-      const u32x4 z = {0, 0, 0, 0};
-      q[c][j] = mine ? *(const u32x4*)(a.q + (s.first + row) * a.qs + (kvh * v.rep + cc % v.rep) * D + 16 * j + 8 * h) : z;
-      if (a.scale2 < 0) q[c][j] ^= 0x80008000u;             // (the scale below is its magnitude)
-      if (a.scale2 == 0) q[c][j] = z;
-    }
+  for (int j = 0; j < NS; ++j) {
+    const u32x4 z = {0, 0, 0, 0};
+    q[j] = mine ? *(const u32x4*)(a.q + (s.first + cc / v.rep) * a.qs + (kvh * v.rep + cc % v.rep) * D + 16 * j + 8 * h) : z;
+    if (a.scale2 < 0) q[j] ^= 0x80008000u;                  // (the scale below is its magnitude)
+    if (a.scale2 == 0) q[j] = z;
   }
   const float scale2 = a.scale2 == 0 ? 1.f : fabsf(a.scale2);
-  f16v o[NC][CB];
-  float m[NC], l[NC];
+  f16v o[CB];
+  float m = -INFINITY, l = 0;
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    m[c] = -INFINITY;
-    l[c] = 0;
-#pragma unroll
-    for (int k = 0; k < CB; ++k) o[c][k] = f16v{};
-  }
+  for (int k = 0; k < CB; ++k) o[k] = f16v{};
 
-  // Staging: a wave's load r takes 64 neighbouring parts, which lie in one page (in the pages of two sixteens of
-  // tokens where a row is but two parts) and one after the other in memory: scalar addresses plus 16 bytes a lane.
-  constexpr int TL = 64 / VP;                               // tokens of a wave's load
+  // Staging: the lanes of a wave take 64 neighbouring parts, which lie in one page (in the pages of two sixteens of tokens
+  // where a row is but two parts) and one after the other in memory: a scalar address, and 16 bytes a lane.  A wave
+  // takes G such groups of keys and the same of values, or, where a tile's keys are fewer parts than threads, one of either.
+  constexpr bool BOTH = T * VP >= N;
+  constexpr int G = BOTH ? T * VP / N : 1, R = BOTH ? 2 * G : 1, TL = 64 / VP, NP = TL > 16 ? 2 : 1;   // loads; tokens of one; their pages
+  static_assert(!BOTH || T * VP % N == 0, "groups of keys and values fall together");
   const int mask = (1 << v.page_shift) - 1;
-  const int64_t bb = paged_block<D, BITS>(v.page_shift);
+  const int64_t page_bytes = paged_block<D, BITS>(v.page_shift) * v.Hkv;
+  const unsigned char* pool = v.pool + paged_block<D, BITS>(v.page_shift) * kvh;
   const int last_page = (s.len - 1) >> v.page_shift;
   const PAGED_CONST int* table = (const PAGED_CONST int*)(v.table + (int64_t)b * v.max_pages);
+  const bool has = BOTH || wave < 2 * T * VP / 64, val0 = !BOTH && wave >= T * VP / 64;   // (else: this wave's load is of values)
   const int ltok = lane / VP, lpart = lane % VP;
+  const int tok0 = (wave * 64 / VP) % T;                    // first token of this wave's first group
+  const uint32_t lcode = lane * 16 % (16 * rb), lscale = (ltok & 15) * sb + lpart * (128 / BITS) / 32;   // (of a sixteen of tokens)
   u32x4 x[R];
   uint32_t xs[R];
-  int page[R][TL > 16 ? 2 : 1];
-  // load r of this wave: keys or values, and its first token
-  auto first_part = [&](int r) { return 64 * (wave + WAVES * r); };
-  auto has = [&](int r) { return N * r + N <= PARTS || first_part(r) < PARTS; };
-  auto is_val = [&](int r) { return N * r >= T * VP || (N * r + N > T * VP && first_part(r) >= T * VP); };
-  auto tok_of = [&](int r) { return first_part(r) / VP % T; };
-  auto pages = [&](int t) {
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-      if (has(r)) {
-#pragma unroll
-        for (int i = 0; i < (TL > 16 ? 2 : 1); ++i) page[r][i] = table[min((t + tok_of(r) + 16 * i) >> v.page_shift, last_page)];
-      }
-  };
-  int page_was[R][TL > 16 ? 2 : 1];                         // of the tile in x
+  int page[G][NP], was[G][NP];                              // of the tile to load, and of the one in x
   bool gone = false;                                        // a page of it is none of the pool's
-  auto load = [&](int t) {
+  auto pages = [&](int t) PAGED_INLINE {
+#pragma unroll
+    for (int r = 0; r < G; ++r)
+#pragma unroll
+      for (int i = 0; i < NP; ++i) page[r][i] = table[min((t + tok0 + r * (N / VP) + 16 * i) >> v.page_shift, last_page)];
+  };
+  auto load = [&](int t) PAGED_INLINE {
     gone = false;
+    if (!has) return;
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-      if (has(r)) {
-        const bool val = is_val(r);
-        const unsigned char* at[TL > 16 ? 2 : 1];           // first code, first scale
-        const unsigned char* sat[TL > 16 ? 2 : 1];
+    for (int r = 0; r < G; ++r) {
+      const unsigned char *at[NP], *sat[NP];                // first key code, first key scale
 #pragma unroll
-        for (int i = 0; i < (TL > 16 ? 2 : 1); ++i) {
-          page_was[r][i] = page[r][i];
-          const bool ok = (unsigned)page[r][i] < (unsigned)v.n_pages;
-          gone |= !ok;
-          const unsigned char* blk = v.pool + ((int64_t)(ok ? page[r][i] : 0) * v.Hkv + kvh) * bb;
-          const int slot = (t + tok_of(r) + 16 * i) & mask;
-          at[i] = blk + ((val ? rb : 0) << v.page_shift) + slot * rb;
-          sat[i] = blk + ((2 * rb + (val ? sb : 0)) << v.page_shift) + slot * sb;
-        }
-        if constexpr (TL > 16) {
-          x[r] = *(const u32x4*)((lane < 32 ? at[0] : at[1]) + (lane & 31) * 16);
-          xs[r] = ((lane < 32 ? sat[0] : sat[1]) + (ltok & 15) * sb)[lpart * (128 / BITS) / 32];
-        } else {
-          x[r] = *(const u32x4*)(at[0] + lane * 16);
-          if constexpr (BITS < 16) xs[r] = (sat[0] + ltok * sb)[lpart * (128 / BITS) / 32];
-        }
+      for (int i = 0; i < NP; ++i) {
+        was[r][i] = page[r][i];
+        const bool ok = (unsigned)page[r][i] < (unsigned)v.n_pages;
+        gone |= !ok;
+        const unsigned char* blk = pool + (ok ? page[r][i] : 0) * page_bytes;
+        const int slot = (t + tok0 + r * (N / VP) + 16 * i) & mask;
+        at[i] = blk + slot * rb + ((val0 ? rb : 0) << v.page_shift);
+        sat[i] = blk + ((2 * rb + (val0 ? sb : 0)) << v.page_shift) + slot * sb;
       }
+#pragma unroll
+      for (int w = 0; w < (BOTH ? 2 : 1); ++w) {            // keys, values
+        const unsigned char* c = at[0];
+        const unsigned char* e = sat[0];
+        if constexpr (NP > 1) {
+          c = lane < 32 ? c : at[1];
+          e = lane < 32 ? e : sat[1];
+        }
+        x[r + w * G] = *(const u32x4*)(c + ((w * rb) << v.page_shift) + lcode);
+        if constexpr (BITS < 16) xs[r + w * G] = e[((w * sb) << v.page_shift) + lscale];
+      }
+    }
   };
   // rows that all columns of the workgroup see whole
   const int wg_lo = paged_lo_of(a, s.base + r1 / v.rep), wg_hi = paged_hi_of(a, s, s.base + r0);
-  auto stage = [&](int t, int buf) {
+  auto stage = [&](int t, int kb, int vb) PAGED_INLINE {
+    if (!has) return;
     const bool plain = t >= wg_lo && t + T <= wg_hi && !gone;
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-      if (has(r)) {
-        const bool val = is_val(r);
-        const int tok = tok_of(r) + ltok;
-        if (__builtin_expect(!plain, 0)) {
-          // values that no row of the tile sees, or of no page, count as zeros; keys of no page as NaN
-          const int pg = TL > 16 && lane >= 32 ? page_was[r][TL > 16 ? 1 : 0] : page_was[r][0];
-          const bool ok = (unsigned)pg < (unsigned)v.n_pages, seen = ok && t + tok < all_hi && t + tok >= all_lo;
-          const u32x4 z = {0, 0, 0, 0}, none = {~0u, ~0u, ~0u, ~0u};
-          if (val) x[r] = seen ? x[r] : z;
-          else if (BITS == 16) x[r] = ok ? x[r] : none;
-          bool odd = false;
-          if constexpr (BITS < 16) {
-            xs[r] = val ? (seen ? xs[r] : 127) : ok ? xs[r] : 255;
-            odd = xs[r] == 255;
-          } else {
+    for (int r = 0; r < R; ++r) {
+      const bool val = BOTH ? r >= G : val0;
+      const int tok = tok0 + (r % G) * (N / VP) + ltok;
+      if (__builtin_expect(!plain, 0)) {
+        // values that no row of the tile sees, or of no page, count as zeros; keys of no page as NaN
+        const int pg = NP > 1 && lane >= 32 ? was[r % G][NP - 1] : was[r % G][0];
+        const bool ok = (unsigned)pg < (unsigned)v.n_pages, seen = ok && t + tok < all_hi && t + tok >= all_lo;
+        const u32x4 z = {0, 0, 0, 0}, none = {~0u, ~0u, ~0u, ~0u};
+        if (val) x[r] = seen ? x[r] : z;
+        else if (BITS == 16) x[r] = ok ? x[r] : none;
+        bool odd = false;
+        if constexpr (BITS < 16) {
+          xs[r] = val ? (seen ? xs[r] : 127) : ok ? xs[r] : 255;
+          odd = xs[r] == 255;
+        } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) odd |= paged_odd<DT>(x[r][e]) || paged_odd<DT>(x[r][e] >> 16);
-          }
-          if (val && odd) odd_tile[buf] = t;
+          for (int e = 0; e < 4; ++e) odd |= paged_odd<DT>(x[r][e]) || paged_odd<DT>(x[r][e] >> 16);
         }
-        u32x4* d = (u32x4*)((val ? lv[buf] + tok * PV : lk[buf] + tok * PK) + lpart * (128 / BITS));
-        if constexpr (BITS == 16) d[0] = x[r];
-        else {
+        if (val && odd) odd_tile[vb] = t;
+      }
+      u32x4* d = (u32x4*)((val ? lv[vb] + tok * PV : lk[kb] + tok * PK) + lpart * (128 / BITS));
+      if constexpr (BITS == 16) d[0] = x[r];
+      else {
 #pragma unroll
-          for (int e = 0; e < 16 / BITS; ++e) {
-            const u32x2 w = {x[r][BITS == 8 ? 2 * e : e], BITS == 8 ? x[r][2 * e + 1] : 0};
-            d[e] = paged_decode8<DT, BITS>(w, paged_scale(xs[r]));
-          }
+        for (int e = 0; e < 16 / BITS; ++e) {
+          const u32x2 w = {x[r][BITS == 8 ? 2 * e : e], BITS == 8 ? x[r][2 * e + 1] : 0};
+          d[e] = paged_decode8<DT, BITS>(w, paged_scale(xs[r]));
         }
       }
+    }
   };
 
-  auto compute = [&](auto masked, int t, int buf) {         // masked: some column does not see some token
-    constexpr bool MASKED = decltype(masked)::value;
-    const unsigned short *kb = lk[buf], *vb = lv[buf];
-    f16v sc[NC][2];
+  // scores of 32 tokens: S^T = K Q^T
+  auto scores = [&](const unsigned short* kb, f16v& sc) PAGED_INLINE {
+    sc = f16v{};
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-#pragma unroll
-      for (int c = 0; c < NC; ++c) sc[c][i] = f16v{};
-#pragma unroll
-      for (int j = 0; j < NS; ++j) {
-        const u32x4 kk = *(const u32x4*)(kb + (32 * i + n) * PK + 16 * j + 8 * h);
-#pragma unroll
-        for (int c = 0; c < NC; ++c) sc[c][i] = paged_mfma32<DT>(kk, q[c][j], sc[c][i]);
-      }
-    }
-    u32x4 p[NC][4];
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      if constexpr (MASKED) {
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const int tok = t + 32 * (e >> 4) + 8 * ((e & 15) >> 2) + 4 * h + (e & 3);
-          sc[c][e >> 4][e & 15] = tok >= lo[c] && tok < hi[c] ? sc[c][e >> 4][e & 15] : -INFINITY;
-        }
-      }
-      float top = sc[c][0][0];
-#pragma unroll
-      for (int e = 1; e < 32; ++e) top = fmaxf(top, sc[c][e >> 4][e & 15]);
-      float mine;
-      const float other = paged_other(top, mine);
-      top = fmaxf(mine, other) * scale2;
-      const bool up = top > m[c] + SLACK || (m[c] == -INFINITY && top > m[c]);
-      if (__any(up)) {
-        const float m2 = up ? top : m[c], f = up ? paged_exp2(m[c] - m2) : 1.f;
-        m[c] = m2;
-        l[c] *= f;
-#pragma unroll
-        for (int k = 0; k < CB; ++k) o[c][k] *= f;
-      }
-      const float ref = paged_chunk_bias<DT>() - (m[c] == -INFINITY ? 0.f : m[c]);
-      float sum = 0;
-#pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        sc[c][e >> 4][e & 15] = paged_exp2(__builtin_fmaf(sc[c][e >> 4][e & 15], scale2, ref));
-        sum += sc[c][e >> 4][e & 15];
-      }
-      l[c] += sum;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) p[c][e >> 2][e & 3] = paged_pair<DT>(sc[c][e >> 3][2 * (e & 7)], sc[c][e >> 3][2 * (e & 7) + 1]);
-    }
-    // values: lane 16 (2 h + i) + j gives the address of token 4 h + j / 4 (and 8 more), channels 16 i + 4 (j % 4) ..
-    const unsigned short* at = vb + (4 * h + ((lane & 15) >> 2)) * PV + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-    const bool fix = MASKED && odd_tile[buf] == t;
-    if (MASKED && fix) {
+    for (int j = 0; j < NS; ++j) sc = paged_mfma32<DT>(*(const u32x4*)(kb + n * PK + 16 * j + 8 * h), q[j], sc);
+  };
+  // O^T += V^T P^T over 32 tokens from t on.  Lane 16 (2 h + i) + j gives the address of token 4 h + j / 4 (and 8 more), channels
+  // 16 i + 4 (j % 4) ..
+  auto values = [&](auto fix, const unsigned short* vb, const u32x4* p, int t) PAGED_INLINE {
+    if constexpr (decltype(fix)::value) {
       // Values that are not finite, and rows that do not see them: 0 times those is not 0.  Rows that see one take it here; the
       // products below find a zero in its place.
 #pragma unroll 1
-      for (int tok = 0; tok < T; ++tok) {
+      for (int tok = 0; tok < 32; ++tok) {
+        uint32_t pw = 0;
+        const int want = (tok >> 3) * 2 + ((tok & 3) >> 1);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          uint32_t pw = 0;
-          const int want = (tok >> 5) * 8 + ((tok & 31) >> 3) * 2 + ((tok & 3) >> 1);
+        for (int e = 0; e < 8; ++e) pw = want == e ? p[e >> 2][e & 3] : pw;
+        pw = __shfl(pw, n + 32 * ((tok >> 2) & 1));
+        const float pf = tok & 1 ? paged_hi<DT>(pw) : paged_lo<DT>(pw);
+        const bool sees = t + tok >= lo && t + tok < hi;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) pw = want == e ? p[c][e >> 2][e & 3] : pw;
-          pw = __shfl(pw, n + 32 * ((tok >> 2) & 1));
-          const float pf = tok & 1 ? paged_hi<DT>(pw) : paged_lo<DT>(pw);
-          const bool sees = t + tok >= lo[c] && t + tok < hi[c];
+        for (int k = 0; k < CB; ++k)
 #pragma unroll
-          for (int k = 0; k < CB; ++k)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const uint32_t bits = vb[tok * PV + 32 * k + 8 * (e >> 2) + 4 * h + (e & 3)];
-              if (sees && paged_odd<DT>(bits)) o[c][k][e] += pf * paged_lo<DT>(bits);
-            }
-        }
+          for (int e = 0; e < 16; ++e) {
+            const uint32_t bits = vb[tok * PV + 32 * k + 8 * (e >> 2) + 4 * h + (e & 3)];
+            if (sees && paged_odd<DT>(bits)) o[k][e] += pf * paged_lo<DT>(bits);
+          }
       }
     }
-    auto products = [&](auto finite) {
+    const unsigned short* from = vb + (4 * h + ((lane & 15) >> 2)) * PV + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int k = 0; k < CB; ++k) {
-          const u32x2 a0 = paged_transposed(at + 16 * j * PV + 32 * k), a1 = paged_transposed(at + (16 * j + 8) * PV + 32 * k);
-          u32x4 vv = {a0[0], a0[1], a1[0], a1[1]};
-          if constexpr (decltype(finite)::value) {
+      for (int k = 0; k < CB; ++k) {
+        const u32x2 a0 = paged_transposed(from + 16 * j * PV + 32 * k), a1 = paged_transposed(from + (16 * j + 8) * PV + 32 * k);
+        u32x4 vv = {a0[0], a0[1], a1[0], a1[1]};
+        if constexpr (decltype(fix)::value) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) vv[e] = paged_finite<DT>(vv[e]);
-          }
-#pragma unroll
-          for (int c = 0; c < NC; ++c) o[c][k] = paged_mfma32<DT>(vv, p[c][j], o[c][k]);
+          for (int e = 0; e < 4; ++e) vv[e] = paged_finite<DT>(vv[e]);
         }
-    };
-    if constexpr (MASKED) {
-      if (fix) products(std::true_type{});
-      else products(std::false_type{});
-    } else products(std::false_type{});
+        o[k] = paged_mfma32<DT>(vv, p[j], o[k]);
+      }
+  };
+  // Half a tile's step: the softmax of 32 tokens (from t on) beside two products that do not depend on it, the next 32 tokens'
+  // scores and the 32 values before.  Those belong to the maximum before this step: O is scaled anew at its end.
+  auto step = [&](auto masked, f16v& sc, f16v& next, const unsigned short* kb, u32x4* p, const u32x4* before, const unsigned short* vb,
+                  int t, int tb, bool odd) PAGED_INLINE {
+    if constexpr (decltype(masked)::value) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int tok = t + 8 * (e >> 2) + 4 * h + (e & 3);
+        sc[e] = tok >= lo && tok < hi ? sc[e] : -INFINITY;
+      }
+    }
+    float top = sc[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) top = fmaxf(top, sc[e]);
+    float own;
+    const float other = paged_other(top, own);
+    top = fmaxf(own, other) * scale2;
+    const bool up = top > m + SLACK || (m == -INFINITY && top > m);
+    const float m2 = up ? top : m, f = up ? paged_exp2(m - m2) : 1.f;
+    const float ref = paged_chunk_bias<DT>() - (m2 == -INFINITY ? 0.f : m2);
+    m = m2;
+    scores(kb, next);
+    float sum = 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      sc[e] = paged_exp2(__builtin_fmaf(sc[e], scale2, ref));
+      sum += sc[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e >> 2][e & 3] = paged_pair<DT>(sc[2 * e], sc[2 * e + 1]);
+    if constexpr (decltype(masked)::value) {
+      if (vb) {
+        if (odd) values(std::true_type{}, vb, before, tb);
+        else values(std::false_type{}, vb, before, tb);
+      }
+    } else values(std::false_type{}, vb, before, tb);
+    asm volatile("" : "+v"(p[0]), "+v"(p[1]), "+v"(sum));   // (before the branch, beside the products, not where they are needed)
+    if (__any(up)) {
+      l *= f;
+#pragma unroll
+      for (int k = 0; k < CB; ++k) o[k] *= f;
+    }
+    l += sum;
   };
 
   // The tiles' order: those that not all columns see whole first (in front of a window's end, then the last tokens'), in a loop
@@ -736,60 +717,80 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
   const int whole_from = max(from, (wg_lo + T - 1) & ~(T - 1)), whole_to = min(to, wg_hi & ~(T - 1));
   const int tiles = from < to ? (to - from + T - 1) / T : 0, whole = max(0, (whole_to - whole_from) / T), partial = tiles - whole;
   const int front = whole ? (whole_from - from) / T : tiles;
-  auto tile_at = [&](int i) { return i < front ? from + i * T : i < partial ? whole_to + (i - front) * T : whole_from + (i - partial) * T; };
-  if (tid < 2) odd_tile[tid] = -1;
+  auto tile_at = [&](int i) PAGED_INLINE { return i < front ? from + i * T : i < partial ? whole_to + (i - front) * T : whole_from + (i - partial) * T; };
+  if (tid < 4) odd_tile[tid] = -1;
   __syncthreads();
+  u32x4 p0[2] = {}, p1[2] = {};
+  f16v s0, s1;
   if (tiles > 0) {
-    pages(tile_at(0));
-    load(tile_at(0));
-    if (tiles > 1) pages(tile_at(1));
-    stage(tile_at(0), 0);
-  }
-  __syncthreads();
-  int i = 0;
-  auto walk = [&](auto masked, int end) {
-    for (; i < end; ++i) {
-      const int t = tile_at(i), buf = i & 1;
-      if (i + 1 < tiles) {
-        load(tile_at(i + 1));
-        if (i + 2 < tiles) pages(tile_at(i + 2));
-      }
-      if (!decltype(masked)::value || (t < some_hi && t + T > some_lo)) compute(masked, t, buf);
-      if (i + 1 < tiles) stage(tile_at(i + 1), buf ^ 1);
-      __syncthreads();
+    int t0 = tile_at(0), t1 = tile_at(1), t2 = tile_at(2), before = 0;   // tiles i, i + 1, i + 2 (where there are such), i - 1
+    pages(t0);
+    load(t0);
+    pages(t1);
+    stage(t0, 0, 0);
+    if (tiles > 1) {
+      load(t1);
+      pages(t2);
+      stage(t1, 1, 1);
     }
-  };
-  walk(std::true_type{}, partial);
-  walk(std::false_type{}, tiles);
-
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int cc = w0 + 32 * c + n;
-    float mine;
-    const float other = paged_other(l[c], mine), sum = mine + other;
-    if (cc >= cols) continue;
-    const int64_t at = (int64_t)(s.first + cc / v.rep) * v.Hq + kvh * v.rep + cc % v.rep;
-    if (a.sp.splits == 1) {
-      const float inv = sum == 0 ? 0.f : 1.f / sum;
-#pragma unroll
-      for (int k = 0; k < CB; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const u32x2 w = {paged_pair<DT>(o[c][k][4 * e] * inv, o[c][k][4 * e + 1] * inv),
-                           paged_pair<DT>(o[c][k][4 * e + 2] * inv, o[c][k][4 * e + 3] * inv)};
-          *(u32x2*)(a.out + at * D + 32 * k + 8 * e + 4 * h) = w;
+    __syncthreads();
+    scores(lk[0], s0);
+    int i = 0, k0 = 0, k1 = 1, k2 = 2;                      // buffers of keys of tiles i, i + 1, i + 2
+    auto walk = [&](auto masked, int end) PAGED_INLINE {
+      constexpr bool M = decltype(masked)::value;
+      for (; i < end; ++i) {
+        const int t3 = M ? tile_at(i + 3) : t2 + T;         // (M: the next may be elsewhere)
+        const bool more = i + 2 < tiles;
+        if (more) {
+          load(t2);
+          pages(t3);
         }
-      if (a.lse && h == 0) a.lse[at] = sum == 0 ? -INFINITY : (m[c] + __log2f(sum) - paged_chunk_bias<DT>()) * 0.69314718055994531f;
-    } else {
-      const int64_t u = (((int64_t)unit * v.Hkv + kvh) * COLS + (cc - c0)) * a.sp.splits + split;
+        // (the keys of a tile that is not there give scores that nothing looks at)
+        const bool ob = M && odd_tile[(i - 1) & 3] == before, oc = M && odd_tile[i & 3] == t0;
+        step(masked, s0, s1, lk[k0] + 32 * PK, p0, p1, M && !i ? nullptr : lv[(i - 1) & 3] + 32 * PV, t0, before + 32, ob);
+        step(masked, s1, s0, lk[k1], p1, p0, lv[i & 3], t0 + 32, t0, oc);
+        if (more) stage(t2, k2, (i + 2) & 3);
+        __syncthreads();
+        const int k = k0;
+        k0 = k1;
+        k1 = k2;
+        k2 = k;
+        before = t0;
+        t0 = t1;
+        t1 = t2;
+        t2 = t3;
+      }
+    };
+    // (the first tile, and the one after a partial one, may have values of a partial tile, or none, before them)
+    walk(std::true_type{}, min(partial + 1, tiles));
+    walk(std::false_type{}, tiles);
+    const int t = tile_at(tiles - 1), vb = (tiles - 1) & 3;
+    if (odd_tile[vb] == t) values(std::true_type{}, lv[vb] + 32 * PV, p1, t + 32);
+    else values(std::false_type{}, lv[vb] + 32 * PV, p1, t + 32);
+  }
+
+  float own;
+  const float other = paged_other(l, own), sum = own + other;
+  if (!mine) return;
+  if (a.sp.splits == 1) {
+    const float inv = sum == 0 ? 0.f : 1.f / sum;
 #pragma unroll
-      for (int k = 0; k < CB; ++k)
+    for (int k = 0; k < CB; ++k)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          *(f4*)(a.sp.acc + u * D + 32 * k + 8 * e + 4 * h) = f4{o[c][k][4 * e], o[c][k][4 * e + 1], o[c][k][4 * e + 2], o[c][k][4 * e + 3]};
-      // (as k_paged_few's: the merge knows one bias)
-      if (h == 0) a.sp.ml[u] = make_float2(m[c] + (paged_bias<DT>() - paged_chunk_bias<DT>()), sum);
-    }
+      for (int e = 0; e < 4; ++e) {
+        const u32x2 w = {paged_pair<DT>(o[k][4 * e] * inv, o[k][4 * e + 1] * inv), paged_pair<DT>(o[k][4 * e + 2] * inv, o[k][4 * e + 3] * inv)};
+        *(u32x2*)(a.out + at * D + 32 * k + 8 * e + 4 * h) = w;
+      }
+    if (a.lse && h == 0) a.lse[at] = sum == 0 ? -INFINITY : (m + __log2f(sum) - paged_chunk_bias<DT>()) * 0.69314718055994531f;
+  } else {
+    const int64_t u = (((int64_t)unit * v.Hkv + kvh) * COLS + (cc - c0)) * a.sp.splits + split;
+#pragma unroll
+    for (int k = 0; k < CB; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *(f4*)(a.sp.acc + u * D + 32 * k + 8 * e + 4 * h) = f4{o[k][4 * e], o[k][4 * e + 1], o[k][4 * e + 2], o[k][4 * e + 3]};
+    // (as k_paged_few's: the merge knows one bias)
+    if (h == 0) a.sp.ml[u] = make_float2(m + (paged_bias<DT>() - paged_chunk_bias<DT>()), sum);
   }
 }
 
@@ -886,7 +887,7 @@ static void launch(const PagedView& v, PagedAsk a, void* scratch, hipStream_t s)
     paged_cut(v, a.window, PAGED_TILE, units, CHUNK_WANT, CHUNK_STEP, rows, &a.sp);
     a.sp.acc = (float*)((char*)scratch + few_bytes(v, D));
     a.sp.ml = (float2*)(a.sp.acc + units * RKV_PAGED_COLS * a.sp.splits * D);
-    k_paged_chunk<D, BITS, DT, 8, 1><<<dim3((unsigned)units, a.sp.splits), 512, 0, s>>>(v, a);
+    k_paged_chunk<D, BITS, DT, 8><<<dim3((unsigned)units, a.sp.splits), 512, 0, s>>>(v, a);
     if (a.sp.splits > 1) k_paged_chunk_merge<D, DT, RKV_PAGED_COLS><<<dim3((unsigned)units, RKV_PAGED_COLS / 4), 256, 0, s>>>(v, a);
   }
 }
