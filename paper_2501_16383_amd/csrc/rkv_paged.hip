@@ -300,7 +300,7 @@ RKV_EXPORT int rkv_paged_scratch(const rkv_paged_config* cfg, const rkv_paged_ba
   PagedView v{};
   const int rc = check_batch(cfg, batch, nullptr, &v);
   if (rc != RKV_OK) return rc;
-  if (scratch_bytes) *scratch_bytes = v.n_rows ? rkv_paged_attention_scratch(v, cfg->head_dim) : 0;
+  if (scratch_bytes) *scratch_bytes = v.n_rows ? rkv_paged_attention_scratch(v, cfg->head_dim, cfg->bits) : 0;
   return RKV_OK;
 }
 
@@ -313,7 +313,7 @@ RKV_EXPORT int rkv_paged_attention(const rkv_paged_config* cfg, const void* dev_
   if ((causal != 0 && causal != 1) || window < 0 || !__builtin_isfinite(scale)) return RKV_EINVAL;
   if (v.n_rows == 0) return RKV_OK;
   if (!dev_pool || !rows_ok(cfg, dev_q, q_stride, cfg->n_q_heads) || !dev_out || ((uintptr_t)dev_out & 15) || ((uintptr_t)dev_lse & 3)) return RKV_EINVAL;
-  const size_t need = rkv_paged_attention_scratch(v, cfg->head_dim);
+  const size_t need = rkv_paged_attention_scratch(v, cfg->head_dim, cfg->bits);
   if (need && (!dev_scratch || ((uintptr_t)dev_scratch & 255) || scratch_bytes < need)) return RKV_EINVAL;
   return rkv_launch_paged_attention(v, cfg->head_dim, cfg->bits, cfg->dtype, dev_q, q_stride, causal, window, scale, dev_out, dev_lse,
                                     dev_scratch, (hipStream_t)stream);

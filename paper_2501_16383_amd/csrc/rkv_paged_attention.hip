@@ -119,19 +119,12 @@ template <int D, int DT> __device__ __forceinline__ void paged_bad_rows(const Pa
 // A workgroup takes up to 16 NB columns of one (sequence, KV head) over one split of its tokens, each wave every
 // fourth tile of 32.  Keys go from memory into the registers of the lanes that feed them to the matrix unit
 // (lane l: token l % 16, a quarter of its channels); values, whose operand runs along the tokens, pass through
-// the wave's own LDS as 16-bit rows and come back transposed.  The next tile's bytes are in flight while
-// one is computed.
-template <int D, int BITS> struct FewTile {
-  static constexpr int KL = D * BITS / 8 / 4 / 16;          // 16-byte loads of a quarter row of keys (0: one of 8 bytes)
-  static constexpr int VP = D * BITS / 8 / 16;              // 16-byte parts of a row of values
-  static constexpr int VL = 32 * VP / 64;                   // loads of a lane for 32 tokens
-  u32x4 k[2][KL ? KL : 1], v[VL];
-  uint32_t ks[2], vs[VL];
-};
-
+// the wave's own LDS as 16-bit rows and come back transposed.  The next tile's values are asked for as soon as
+// these are in LDS, its keys as soon as these are multiplied.
 template <int D, int BITS, int DT, int NB>
-__global__ __launch_bounds__(256) void k_paged_few(PagedView v, PagedAsk a) {
-  using Tile = FewTile<D, BITS>;
+__global__ __launch_bounds__(256, NB == 1 ? 3 : 2) void k_paged_few(PagedView v, PagedAsk a) {
+  constexpr int KL = D * BITS / 8 / 4 / 16;                 // 16-byte loads of a quarter row of keys (0: one of 8 bytes)
+  constexpr int VP = D * BITS / 8 / 16, VL = 32 * VP / 64;  // 16-byte parts of a row of values; loads of a lane for 32 tokens
   constexpr int rb = paged_row<D, BITS>(), sb = paged_srow<D, BITS>();
   constexpr int PITCH = D + 16;                             // 16-bit elements between two tokens' values in LDS
   constexpr int CB = D / 16, NK = D / 32;
@@ -186,71 +179,101 @@ __global__ __launch_bounds__(256) void k_paged_few(PagedView v, PagedAsk a) {
   }
   unsigned short* vl = lds + wave * 32 * PITCH;
   const int mask = (1 << v.page_shift) - 1;
-  const int64_t bb = paged_block<D, BITS>(v.page_shift);
+  const int64_t page_bytes = paged_block<D, BITS>(v.page_shift) * v.Hkv;
+  const unsigned char* pool = v.pool + paged_block<D, BITS>(v.page_shift) * kvh;
   const int last_page = (s.len - 1) >> v.page_shift;        // (len > 0 where there is a tile at all)
+  const PAGED_CONST int* table = (const PAGED_CONST int*)(v.table + (int64_t)b * v.max_pages);
+  u32x4 kx[2][KL ? KL : 1], vx[VL];                         // bytes of the tile to come
+  uint32_t ks[2], vs[VL];
+  int page[2];                                              // of its two sixteens of tokens
 
-  auto pages = [&](int t, int* p) PAGED_INLINE {
+  auto pages = [&](int t) PAGED_INLINE {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) p[i] = v.table[(int64_t)b * v.max_pages + min((t + 16 * i) >> v.page_shift, last_page)];
+    for (int i = 0; i < 2; ++i) page[i] = table[min((t + 16 * i) >> v.page_shift, last_page)];
   };
-  auto load = [&](int t, const int* p, Tile& x) PAGED_INLINE {
-    const unsigned char* blk[2];
-    bool ok[2];
+  auto block = [&](int i, bool& ok) PAGED_INLINE {
+    ok = (unsigned)page[i] < (unsigned)v.n_pages;
+    return pool + (ok ? page[i] : 0) * page_bytes;
+  };
+  auto load_keys = [&](int t) PAGED_INLINE {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      ok[i] = (unsigned)p[i] < (unsigned)v.n_pages;
-      blk[i] = v.pool + ((int64_t)(ok[i] ? p[i] : 0) * v.Hkv + kvh) * bb;
+      bool ok;
+      const unsigned char* blk = block(i, ok);
       const int slot = (t + 16 * i) & mask;
-      const unsigned char* kp = blk[i] + (slot + n) * rb + (BITS == 16 ? 16 * g : g * (rb / 4));
-      if constexpr (Tile::KL == 0) {
+      const unsigned char* kp = blk + slot * rb + (n * rb + (BITS == 16 ? 16 * g : g * (rb / 4)));
+      if constexpr (KL == 0) {
         const u32x2 w = *(const u32x2*)kp;
-        x.k[i][0] = u32x4{w[0], w[1], 0, 0};
+        kx[i][0] = u32x4{w[0], w[1], 0, 0};
       } else {
 #pragma unroll
-        for (int j = 0; j < Tile::KL; ++j) x.k[i][j] = *(const u32x4*)(kp + (BITS == 16 ? 64 : 16) * j);
+        for (int j = 0; j < KL; ++j) kx[i][j] = *(const u32x4*)(kp + (BITS == 16 ? 64 : 16) * j);
       }
       if constexpr (BITS < 16) {
-        x.ks[i] = blk[i][((2 * rb) << v.page_shift) + (slot + n) * sb + (D == 128 ? g : g >> 1)];
-        if (!ok[i]) x.ks[i] = 255;
-      } else if (!ok[i]) {
+        ks[i] = (blk + ((2 * rb) << v.page_shift) + slot * sb)[n * sb + (D == 128 ? g : g >> 1)];
+        if (!ok) ks[i] = 255;                               // keys of no page: NaN
+      } else if (!ok) {
 #pragma unroll
-        for (int j = 0; j < Tile::KL; ++j) x.k[i][j] = u32x4{~0u, ~0u, ~0u, ~0u};
+        for (int j = 0; j < KL; ++j) kx[i][j] = u32x4{~0u, ~0u, ~0u, ~0u};
       }
     }
+  };
+  auto load_values = [&](int t) PAGED_INLINE {
+    constexpr int TL = 64 / VP;                             // tokens of a wave's load: of one sixteen, or (D = 64, 4 bits) of both
+    bool ok[2];
+    const unsigned char *at[2], *sat[2];
 #pragma unroll
-    for (int r = 0; r < Tile::VL; ++r) {
-      const int ci = r * 64 + lane, tok = ci / Tile::VP, part = ci % Tile::VP;
-      const int gi = 64 / Tile::VP <= 16 ? (r * 64 / Tile::VP) / 16 : tok >> 4;   // which sixteen tokens
-      const unsigned char* base = 64 / Tile::VP <= 16 ? blk[gi] : gi ? blk[1] : blk[0];
-      const bool fine = 64 / Tile::VP <= 16 ? ok[gi] : gi ? ok[1] : ok[0];
-      const int slot = ((t + 16 * gi) & mask) + (tok & 15);
-      const u32x4 z = {0, 0, 0, 0};
-      // a value row that no row sees, or of no page, counts as zeros: weight 0 times whatever lies there must be 0
-      const bool seen = fine && t + tok < all_hi && t + tok >= all_lo;
-      x.v[r] = seen ? *(const u32x4*)(base + ((int64_t)rb << v.page_shift) + slot * rb + part * 16) : z;
-      if constexpr (BITS < 16) x.vs[r] = seen ? base[((2 * rb + sb) << v.page_shift) + slot * sb + part * (128 / BITS) / 32] : 127;
+    for (int i = 0; i < 2; ++i) {
+      const unsigned char* blk = block(i, ok[i]);
+      const int slot = (t + 16 * i) & mask;
+      at[i] = blk + (rb << v.page_shift) + slot * rb;
+      sat[i] = blk + ((2 * rb + sb) << v.page_shift) + slot * sb;
+    }
+    const bool inside = t >= all_lo && t + 32 <= all_hi && ok[0] && ok[1];
+#pragma unroll
+    for (int r = 0; r < VL; ++r) {
+      const int tok = r * TL + lane / VP, part = lane % VP; // token in the tile
+      const int i = r * TL / 16;
+      const unsigned char* c = TL <= 16 ? at[i] : lane < 32 ? at[0] : at[1];
+      const unsigned char* e = TL <= 16 ? sat[i] : lane < 32 ? sat[0] : sat[1];
+      vx[r] = *(const u32x4*)(c + ((tok & 15) * rb + part * 16));
+      if constexpr (BITS < 16) vs[r] = e[(tok & 15) * sb + part * (128 / BITS) / 32];
+      if (!inside) {
+        // a value row that no row sees, or of no page, counts as zeros: weight 0 times whatever lies there must be 0
+        const bool seen = (TL <= 16 ? ok[i] : lane < 32 ? ok[0] : ok[1]) && t + tok < all_hi && t + tok >= all_lo;
+        if (!seen) vx[r] = u32x4{0, 0, 0, 0};
+        if (BITS < 16 && !seen) vs[r] = 127;
+      }
     }
   };
-  auto compute = [&](int t, const Tile& x) PAGED_INLINE {
+  auto compute = [&](int t, bool more) PAGED_INLINE {         // tile t; more: tile t + 128 is this wave's next
+    const bool whole = t >= full_lo && t + 32 <= full_hi;   // every row sees every token
+    const bool mixed_rows = !whole && rows > 1;             // ... or some do
     // values to LDS as 16-bit rows
     bool odd = false;                                       // holds infinities or NaN
 #pragma unroll
-    for (int r = 0; r < Tile::VL; ++r) {
-      const int ci = r * 64 + lane, tok = ci / Tile::VP, part = ci % Tile::VP;
+    for (int r = 0; r < VL; ++r) {
+      const int ci = r * 64 + lane, tok = ci / VP, part = ci % VP;
       u32x4* d = (u32x4*)(vl + tok * PITCH + part * (128 / BITS));
       if constexpr (BITS == 16) {
-        d[0] = x.v[r];
+        d[0] = vx[r];
+        if (mixed_rows) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) odd |= paged_odd<DT>(x.v[r][e]) || paged_odd<DT>(x.v[r][e] >> 16);
+          for (int e = 0; e < 4; ++e) odd |= paged_odd<DT>(vx[r][e]) || paged_odd<DT>(vx[r][e] >> 16);
+        }
       } else {
-        const float sc = paged_scale(x.vs[r]);
-        odd |= x.vs[r] == 255;
+        const float sc = paged_scale(vs[r]);
+        odd |= vs[r] == 255;
 #pragma unroll
         for (int e = 0; e < 16 / BITS; ++e) {
-          const u32x2 w = {x.v[r][BITS == 8 ? 2 * e : e], BITS == 8 ? x.v[r][2 * e + 1] : 0};
+          const u32x2 w = {vx[r][BITS == 8 ? 2 * e : e], BITS == 8 ? vx[r][2 * e + 1] : 0};
           d[e] = paged_decode8<DT, BITS>(w, sc);
         }
       }
+    }
+    if (more) {
+      pages(t + 128);
+      load_values(t + 128);
     }
     // scores
     f4 sc[NB][2];
@@ -259,11 +282,11 @@ __global__ __launch_bounds__(256) void k_paged_few(PagedView v, PagedAsk a) {
       u32x4 kk[NK];
 #pragma unroll
       for (int j = 0; j < NK; ++j) {
-        if constexpr (BITS == 16) kk[j] = x.k[i][j];
+        if constexpr (BITS == 16) kk[j] = kx[i][j];
         else {
           const int w = j * (BITS / 4);                     // dword of the lane's codes
-          const u32x2 c = {x.k[i][w / 4][w % 4], BITS == 8 ? x.k[i][w / 4][(w % 4) + 1 & 3] : 0};
-          kk[j] = paged_decode8<DT, BITS>(c, paged_scale(x.ks[i]));
+          const u32x2 c = {kx[i][w / 4][w % 4], BITS == 8 ? kx[i][w / 4][(w % 4) + 1 & 3] : 0};
+          kk[j] = paged_decode8<DT, BITS>(c, paged_scale(ks[i]));
         }
       }
 #pragma unroll
@@ -273,7 +296,7 @@ __global__ __launch_bounds__(256) void k_paged_few(PagedView v, PagedAsk a) {
         for (int j = 0; j < NK; ++j) sc[c][i] = paged_mfma16<DT>(kk[j], q[c][j], sc[c][i]);
       }
     }
-    const bool whole = t >= full_lo && t + 32 <= full_hi;   // every row sees every token
+    if (more) load_keys(t + 128);
     u32x4 p[NB];
 #pragma unroll
     for (int c = 0; c < NB; ++c) {
@@ -306,7 +329,7 @@ __global__ __launch_bounds__(256) void k_paged_few(PagedView v, PagedAsk a) {
       for (int e = 0; e < 4; ++e) p[c][e] = paged_pair<DT>(w[2 * e], w[2 * e + 1]);
     }
     wave_lds_fence();
-    if (!whole && rows > 1 && __any(odd)) {
+    if (mixed_rows && __any(odd)) {
       // A value that is not finite, and rows that do not see it: 0 times it is not 0.  Rows that see it take it here; the
       // products below find a zero in its place, and give the other rows the bits that they always have.
 #pragma unroll 1
@@ -347,29 +370,13 @@ __global__ __launch_bounds__(256) void k_paged_few(PagedView v, PagedAsk a) {
     wave_lds_fence();
   };
 
-  {
-    const int first = from + 32 * wave;
-    int pg[2], pn[2];
-    Tile x, y;
-    if (first < to) {
-      pages(first, pg);
-      load(first, pg, x);
-      if (first + 128 < to) pages(first + 128, pn);
-    }
-    for (int t = first; t < to; t += 256) {
-      if (t + 128 < to) {
-        load(t + 128, pn, y);
-        if (t + 256 < to) pages(t + 256, pg);
-      }
-      compute(t, x);
-      if (t + 128 >= to) break;
-      if (t + 256 < to) {
-        load(t + 256, pg, x);
-        if (t + 384 < to) pages(t + 384, pn);
-      }
-      compute(t + 128, y);
-    }
+  const int first = from + 32 * wave;
+  if (first < to) {
+    pages(first);
+    load_values(first);
+    load_keys(first);
   }
+  for (int t = first; t < to; t += 128) compute(t, t + 128 < to);
 
   // the four waves meet
   float* os = (float*)lds;
@@ -794,6 +801,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
   }
 }
 
+// The splits of k_paged_chunk together: they are few.  A lane takes four channels of a column.
 template <int D, int DT, int COLS>
 __global__ __launch_bounds__(256) void k_paged_chunk_merge(PagedView v, PagedAsk a) {
   const int kvh = blockIdx.x % v.Hkv, unit = blockIdx.x / v.Hkv;
@@ -801,13 +809,35 @@ __global__ __launch_bounds__(256) void k_paged_chunk_merge(PagedView v, PagedAsk
   const int b = paged_find_tile(v, a.few, COLS, unit, c0);
   if (b >= v.n_seqs) return;
   const PagedSeq s = paged_seq(v, b);
-  const int c = blockIdx.y * 4 + (threadIdx.x >> 6), cc = c0 + c, cols = (s.last - s.first) * v.rep;
-  if (s.bad || cc >= cols) return;
+  const int cols = (s.last - s.first) * v.rep;
+  if (s.bad) return;
   const int lo = paged_lo_of(a, s.base + c0 / v.rep) & ~(PAGED_TILE - 1);
   const int hi = paged_hi_of(a, s, s.base + (min(c0 + COLS, cols) - 1) / v.rep);
   const int n = max(1, (hi - lo + a.sp.chunk - 1) / a.sp.chunk);
-  paged_join<D, DT>(a, (((int64_t)unit * v.Hkv + kvh) * COLS + c) * a.sp.splits, n,
-                    (int64_t)(s.first + cc / v.rep) * v.Hq + kvh * v.rep + cc % v.rep);
+  constexpr int LANES = D / 4, STEP = 256 / LANES;          // of a column; columns at a time
+  const int ch = threadIdx.x % LANES * 4;
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const int c = (blockIdx.y * 2 + r) * STEP + threadIdx.x / LANES;
+    if (c0 + c >= cols) return;
+    const int64_t u0 = (((int64_t)unit * v.Hkv + kvh) * COLS + c) * a.sp.splits;
+    float mm = -INFINITY, sum = 0;
+    for (int i = 0; i < n; ++i) mm = fmaxf(mm, a.sp.ml[u0 + i].x);
+    const float ref = mm == -INFINITY ? 0.f : mm;
+    f4 acc = {0, 0, 0, 0};
+    for (int i = 0; i < n; ++i) {
+      const float2 ml = a.sp.ml[u0 + i];
+      const f4 x = *(const f4*)(a.sp.acc + (u0 + i) * D + ch);
+      const float f = paged_exp2(ml.x - ref);
+      sum += f * ml.y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += f * x[e];
+    }
+    const int64_t at = (int64_t)(s.first + (c0 + c) / v.rep) * v.Hq + kvh * v.rep + (c0 + c) % v.rep;
+    const float inv = sum == 0 ? 0.f : 1.f / sum;
+    *(u32x2*)(a.out + at * D + ch) = u32x2{paged_pair<DT>(acc[0] * inv, acc[1] * inv), paged_pair<DT>(acc[2] * inv, acc[3] * inv)};
+    if (a.lse && ch == 0) a.lse[at] = paged_lse<DT>(mm, sum);
+  }
 }
 
 // ---- host side ---------------------------------------------------------------------------------
@@ -836,11 +866,12 @@ static size_t paged_cut_bytes(const PagedView& v, int64_t units, int64_t want, i
   return n > 1 ? (size_t)units * cols * n * (D + 2) * 4 : 0;
 }
 
-// k_paged_few: a unit is a (sequence, KV head); two workgroups for each compute unit, splits of at least 128 tokens (32 for
-// each wave)
+// k_paged_few: a unit is a (sequence, KV head); splits of at least 128 tokens (32 for each wave).  Two workgroups for each
+// compute unit have enough bytes in flight, and four where a row is 64 bytes or less (32768 tokens, 32 heads, 4 bits: 31.0 us with
+// four, 36.6 with two; 8 x 4096 tokens, 8 heads, 8 bits: 20.5 with two, 24.5 with four).
 static int64_t few_units(const PagedView& v) { return (int64_t)v.n_seqs * v.Hkv; }
 static int few_cols(const PagedView& v) { return (int64_t)v.max_new * v.rep <= 16 ? 16 : 32; }
-#define FEW_WANT (2 * RKV_PAGED_CUS)
+static int64_t few_want(int D, int bits) { return (D * bits <= 512 ? 4 : 2) * RKV_PAGED_CUS; }
 #define FEW_STEP 128
 // k_paged_chunk: a unit is a tile of columns and a KV head; a workgroup for each compute unit, splits of at least 512 tokens
 static int64_t chunk_units(const PagedView& v) {
@@ -854,17 +885,17 @@ static bool has_few(const PagedView& v) { return v.n_seqs > 1 || (int64_t)v.max_
 static bool has_chunk(const PagedView& v) { return (int64_t)v.max_new * v.rep > RKV_PAGED_FEW; }
 
 // work space: k_paged_few's partial results, then k_paged_chunk's
-static size_t few_bytes(const PagedView& v, int D) {
-  const size_t n = has_few(v) ? paged_cut_bytes(v, few_units(v), FEW_WANT, FEW_STEP, few_cols(v), D) : 0;
+static size_t few_bytes(const PagedView& v, int D, int bits) {
+  const size_t n = has_few(v) ? paged_cut_bytes(v, few_units(v), few_want(D, bits), FEW_STEP, few_cols(v), D) : 0;
   return (n + 255) & ~(size_t)255;
 }
-size_t rkv_paged_attention_scratch(const PagedView& v, int D) {
-  return few_bytes(v, D) + (has_chunk(v) ? paged_cut_bytes(v, chunk_units(v), CHUNK_WANT, CHUNK_STEP, RKV_PAGED_COLS, D) : 0);
+size_t rkv_paged_attention_scratch(const PagedView& v, int D, int bits) {
+  return few_bytes(v, D, bits) + (has_chunk(v) ? paged_cut_bytes(v, chunk_units(v), CHUNK_WANT, CHUNK_STEP, RKV_PAGED_COLS, D) : 0);
 }
 
 template <int D, int BITS, int DT, int NB>
 static void launch_few(const PagedView& v, PagedAsk a, void* scratch, hipStream_t s) {
-  paged_cut(v, a.window, 32, few_units(v), FEW_WANT, FEW_STEP, RKV_PAGED_FEW, &a.sp);
+  paged_cut(v, a.window, 32, few_units(v), few_want(D, BITS), FEW_STEP, RKV_PAGED_FEW, &a.sp);
   a.sp.acc = (float*)scratch;
   a.sp.ml = (float2*)(a.sp.acc + few_units(v) * (16 * NB) * a.sp.splits * D);
   k_paged_few<D, BITS, DT, NB><<<dim3(a.sp.splits, v.Hkv, v.n_seqs), 256, 0, s>>>(v, a);
@@ -885,10 +916,10 @@ static void launch(const PagedView& v, PagedAsk a, void* scratch, hipStream_t s)
     // (rows of a unit; without `causal` its first row sees all behind it)
     const int rows = a.causal && v.max_new > RKV_PAGED_COLS ? RKV_PAGED_COLS : v.max_new;
     paged_cut(v, a.window, PAGED_TILE, units, CHUNK_WANT, CHUNK_STEP, rows, &a.sp);
-    a.sp.acc = (float*)((char*)scratch + few_bytes(v, D));
+    a.sp.acc = (float*)((char*)scratch + few_bytes(v, D, BITS));
     a.sp.ml = (float2*)(a.sp.acc + units * RKV_PAGED_COLS * a.sp.splits * D);
     k_paged_chunk<D, BITS, DT, 8><<<dim3((unsigned)units, a.sp.splits), 512, 0, s>>>(v, a);
-    if (a.sp.splits > 1) k_paged_chunk_merge<D, DT, RKV_PAGED_COLS><<<dim3((unsigned)units, RKV_PAGED_COLS / 4), 256, 0, s>>>(v, a);
+    if (a.sp.splits > 1) k_paged_chunk_merge<D, DT, RKV_PAGED_COLS><<<dim3((unsigned)units, RKV_PAGED_COLS * D / 2048), 256, 0, s>>>(v, a);
   }
 }
 
