@@ -124,12 +124,12 @@ def load_library():
     lib.rkv_import_codes.argtypes = [vp, i32] + [vp] * 7
     lib.rkv_export_sinks.argtypes = [vp] * 6
     lib.rkv_layout_locate.argtypes = [cfgp, i32, i32, i32, i32, C.POINTER(sz), C.POINTER(i32), C.POINTER(sz)]
-    pagedp, batchp, i64 = C.POINTER(_CPagedConfig), C.POINTER(_CPagedBatch), C.c_int64
-    lib.rkv_paged_sizes.argtypes = [pagedp, C.POINTER(sz)]
-    lib.rkv_paged_append.argtypes = [pagedp, vp, batchp, vp, i64, vp, i64, vp]
-    lib.rkv_paged_read.argtypes = [pagedp, vp, batchp, vp, i64, vp, i64, vp]
-    lib.rkv_paged_scratch.argtypes = [pagedp, batchp, C.POINTER(sz)]
-    lib.rkv_paged_attention.argtypes = [pagedp, vp, batchp, vp, i64, i32, i32, C.c_float, vp, vp, vp, sz, vp]
+    i64 = C.c_int64                                            # (structures by their address: the binding keeps them)
+    lib.rkv_paged_sizes.argtypes = [vp, vp]
+    lib.rkv_paged_append.argtypes = [vp, vp, vp, vp, i64, vp, i64, vp]
+    lib.rkv_paged_read.argtypes = [vp, vp, vp, vp, i64, vp, i64, vp]
+    lib.rkv_paged_scratch.argtypes = [vp, vp, vp]
+    lib.rkv_paged_attention.argtypes = [vp, vp, vp, vp, i64, i32, i32, C.c_float, vp, vp, vp, sz, vp]
     lib.rkv_strerror.argtypes = [C.c_int]
     lib.rkv_strerror.restype = C.c_char_p
     for name in EXPORTS:
@@ -155,6 +155,15 @@ def _stream() -> int:
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     except AttributeError:                                     # names torch does not promise to keep
         return torch.cuda.current_stream().cuda_stream
+
+
+def _device() -> int:
+    """Index of the current device."""
+    import torch
+    try:
+        return torch._C._cuda_getDevice()
+    except AttributeError:
+        return torch.cuda.current_device()
 
 
 def _dev(t, dtype, what: str):

@@ -2,9 +2,9 @@
 from __future__ import annotations
 
 import ctypes as C
-from dataclasses import dataclass
+from dataclasses import dataclass, replace
 
-from .binding import _check, _CPagedBatch, _CPagedConfig, _dev, _ptr, _stream, load_library
+from .binding import _check, _CPagedBatch, _CPagedConfig, _dev, _device, _stream, load_library
 
 
 @dataclass
@@ -33,27 +33,34 @@ class RkvPagedBatch:
     """rkv_paged_batch: the sequences of a call and their new rows.
 
     page_table [n_seqs, max_pages], row_start [n_seqs + 1] and lengths [n_seqs] are int32 tensors on the device, read by every
-    call anew (and by every replay of a captured one); n_rows, max_new and max_len are the host's bounds on them."""
+    call anew (and by every replay of a captured one); n_rows, max_new and max_len are the host's bounds on them (n_rows
+    and the tables' capacity where not given).  The object is fixed: a batch of other bounds or tensors is another object."""
+
+    __slots__ = ("page_table", "row_start", "lengths", "device", "n_rows", "_c")
 
     def __init__(self, page_table, row_start, lengths, n_rows: int, max_new: int = None, max_len: int = None):
         import torch
         if page_table is None or row_start is None or lengths is None:
             raise TypeError("page_table, row_start and lengths are needed")
-        self.page_table = _dev(page_table, torch.int32, "page_table")
-        self.row_start = _dev(row_start, torch.int32, "row_start")
-        self.lengths = _dev(lengths, torch.int32, "lengths")
+        page_table, row_start = _dev(page_table, torch.int32, "page_table"), _dev(row_start, torch.int32, "row_start")
+        lengths = _dev(lengths, torch.int32, "lengths")
         if page_table.dim() != 2 or row_start.shape != (page_table.shape[0] + 1,) or lengths.shape != page_table.shape[:1]:
             raise ValueError("page_table must be [n_seqs, max_pages], row_start [n_seqs + 1], lengths [n_seqs]")
         if row_start.device != page_table.device or lengths.device != page_table.device:
             raise ValueError("page_table, row_start and lengths must be on one device")
-        self.device = page_table.device
-        self.n_rows, self.max_new, self.max_len = n_rows, max_new, max_len
+        self.page_table, self.row_start, self.lengths = page_table, row_start, lengths
+        self.device, self.n_rows = page_table.device, n_rows
+        n_seqs, max_pages = page_table.shape
+        self._c = _CPagedBatch(page_table.data_ptr(), row_start.data_ptr(), lengths.data_ptr(), n_seqs, max_pages, n_rows,
+                               n_rows if max_new is None else max_new, -1 if max_len is None else max_len)
 
     def to_c(self, cfg: RkvPagedConfig) -> _CPagedBatch:
-        n_seqs, max_pages = self.page_table.shape
-        return _CPagedBatch(self.page_table.data_ptr(), self.row_start.data_ptr(), self.lengths.data_ptr(), n_seqs, max_pages, self.n_rows,
-                            self.n_rows if self.max_new is None else self.max_new,
-                            min(max_pages * cfg.page_tokens, 1 << 30) if self.max_len is None else self.max_len)
+        """The C structure, for a cache of this configuration."""
+        c = self._c
+        if c.max_len != -1:
+            return c
+        return _CPagedBatch(c.dev_page_table, c.dev_row_start, c.dev_lengths, c.n_seqs, c.max_pages, c.n_rows, c.max_new,
+                            min(c.max_pages * cfg.page_tokens, 1 << 30))
 
 
 class RkvPagedCache:
@@ -62,7 +69,7 @@ class RkvPagedCache:
 
     def __init__(self, cfg: RkvPagedConfig, device="cuda:0", mem=None):
         import torch
-        self.cfg, self.lib = cfg, load_library()
+        self.cfg, self.lib = replace(cfg), load_library()
         self.device = torch.device(device)
         if self.device.type == "cuda" and self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
@@ -74,66 +81,75 @@ class RkvPagedCache:
             raise ValueError(f"mem must hold {n} bytes on {self.device}")
         self.dtype = torch.bfloat16 if cfg.dtype else torch.float16
         self._c = cfg.to_c()
+        # (what every call needs again; a call's own time is a few microseconds)
+        self._at, self._mem_at = C.byref(self._c), mem.data_ptr()
+        self._torch, self._index = torch, self.device.index
 
     def _rows(self, t, heads: int, n_rows: int, what: str):
         """Pointer and row stride of a tensor [n_rows, heads, head_dim] whose heads are dense."""
-        import torch
         D = self.cfg.head_dim
-        if not isinstance(t, torch.Tensor) or t.dtype != self.dtype or t.device != self.device:
+        if not isinstance(t, self._torch.Tensor) or t.dtype is not self.dtype or t.device != self.device:
             raise TypeError(f"{what} must be a tensor of dtype {self.dtype} on {self.device}")
         if t.shape != (n_rows, heads, D):
             raise ValueError(f"{what} must be [{n_rows}, {heads}, {D}]")
-        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != D):
+        s = t.stride()
+        if s[2] != 1 or (s[1] != D and heads > 1):
             raise ValueError(f"{what} must have its heads side by side")
-        return t.data_ptr(), t.stride(0) if n_rows > 1 else heads * D
+        return t.data_ptr(), s[0] if n_rows > 1 else heads * D
 
-    def _call(self, batch, name, *args):
+    def _call(self, function, name, *args):
         """One call of the library with the cache's device current."""
-        import torch
+        if _device() == self._index:
+            rc = function(self._at, self._mem_at, *args, _stream())
+        else:
+            with self._torch.cuda.device(self.device):
+                rc = function(self._at, self._mem_at, *args, _stream())
+        if rc:
+            _check(rc, name)
+
+    def _batch(self, batch):
         if batch.device != self.device:
             raise ValueError(f"the batch must be on {self.device}")
-        cb = batch.to_c(self.cfg)
-        if torch.cuda.current_device() == self.device.index:
-            return self._go(name, cb, *args)
-        with torch.cuda.device(self.device):
-            return self._go(name, cb, *args)
-
-    def _go(self, name, cb, *args):
-        _check(getattr(self.lib, name)(C.byref(self._c), self.mem.data_ptr(), C.byref(cb), *args, _stream()), name)
+        return C.byref(batch.to_c(self.cfg))
 
     def append(self, k, v, batch: RkvPagedBatch):
         """rkv_paged_append: k, v [n_rows, n_kv_heads, head_dim] of the cache's type (rows may be strided)."""
         h, n = self.cfg.n_kv_heads, batch.n_rows
-        self._call(batch, "rkv_paged_append", *self._rows(k, h, n, "k"), *self._rows(v, h, n, "v"))
+        kp, ks = self._rows(k, h, n, "k")
+        vp, vs = self._rows(v, h, n, "v")
+        self._call(self.lib.rkv_paged_append, "rkv_paged_append", self._batch(batch), kp, ks, vp, vs)
 
     def read(self, batch: RkvPagedBatch, k=None, v=None):
         """rkv_paged_read: the rows' keys and values as the cache holds them, into k and v where given."""
-        import torch
-        h, n = self.cfg.n_kv_heads, batch.n_rows
-        shape = (n, h, self.cfg.head_dim)
-        k = torch.empty(shape, dtype=self.dtype, device=self.device) if k is None else k
-        v = torch.empty(shape, dtype=self.dtype, device=self.device) if v is None else v
-        self._call(batch, "rkv_paged_read", *self._rows(k, h, n, "k"), *self._rows(v, h, n, "v"))
+        empty, n, h, D = self._torch.empty, batch.n_rows, self.cfg.n_kv_heads, self.cfg.head_dim
+        k = empty((n, h, D), dtype=self.dtype, device=self.device) if k is None else k
+        v = empty((n, h, D), dtype=self.dtype, device=self.device) if v is None else v
+        kp, ks = self._rows(k, h, n, "k")
+        vp, vs = self._rows(v, h, n, "v")
+        self._call(self.lib.rkv_paged_read, "rkv_paged_read", self._batch(batch), kp, ks, vp, vs)
         return k, v
 
     def attention(self, q, batch: RkvPagedBatch, causal: bool = True, window: int = 0, scale: float = None, out=None, lse=None,
                   want_lse: bool = False):
         """rkv_paged_attention: q [n_rows, n_q_heads, head_dim] -> out of the same shape and type (and lse [n_rows, n_q_heads]
         fp32).  Work space is allocated for each call on its stream, so that calls may overlap."""
-        import torch
-        cfg, n = self.cfg, batch.n_rows
+        torch, cfg, n, dev = self._torch, self.cfg, batch.n_rows, self.device
         qp, qs = self._rows(q, cfg.n_q_heads, n, "q")
         if out is None:
-            out = torch.empty((n, cfg.n_q_heads, cfg.head_dim), dtype=self.dtype, device=self.device)
-        elif _dev(out, self.dtype, "out").shape != q.shape or out.device != self.device:
+            out = torch.empty((n, cfg.n_q_heads, cfg.head_dim), dtype=self.dtype, device=dev)
+        elif _dev(out, self.dtype, "out").shape != q.shape or out.device != dev:
             raise ValueError("out must be a tensor like q")
-        if lse is None and want_lse:
-            lse = torch.empty((n, cfg.n_q_heads), dtype=torch.float32, device=self.device)
-        elif lse is not None and (_dev(lse, torch.float32, "lse").shape != (n, cfg.n_q_heads) or lse.device != self.device):
+        if lse is None:
+            lse = torch.empty((n, cfg.n_q_heads), dtype=torch.float32, device=dev) if want_lse else None
+        elif _dev(lse, torch.float32, "lse").shape != (n, cfg.n_q_heads) or lse.device != dev:
             raise ValueError("lse must be [n_rows, n_q_heads]")
-        need, cb = C.c_size_t(0), batch.to_c(cfg)
-        _check(self.lib.rkv_paged_scratch(C.byref(self._c), C.byref(cb), C.byref(need)), "rkv_paged_scratch")
-        scratch = torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None
-        self._call(batch, "rkv_paged_attention", qp, qs, int(causal), window, cfg.head_dim ** -0.5 if scale is None else scale, out.data_ptr(),
-                   _ptr(lse), _ptr(scratch), need.value)
+        cb, need = self._batch(batch), C.c_size_t()
+        rc = self.lib.rkv_paged_scratch(self._at, cb, C.byref(need))
+        if rc:
+            _check(rc, "rkv_paged_scratch")
+        need = need.value
+        scratch = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        self._call(self.lib.rkv_paged_attention, "rkv_paged_attention", cb, qp, qs, 1 if causal else 0, window,
+                   cfg.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
+                   scratch.data_ptr() if need else None, need)
         return (out, lse) if want_lse else out
