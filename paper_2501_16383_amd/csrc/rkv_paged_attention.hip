@@ -7,6 +7,7 @@
 // the four (eight) weights a lane gets from the first product are, in their order, an operand of the second.
 // (Which token is which index of the sum is free as long as both operands agree.)  Weights are powers of two of
 // scores in fp32; the sum of weights is taken in fp32 from unrounded weights.
+#include <cfloat>
 #include <type_traits>
 
 #include "rkv_mfma_ops.h"
@@ -36,6 +37,15 @@ template <int DT> __device__ __forceinline__ f16v paged_mfma32(u32x4 a, u32x4 b,
 __device__ __forceinline__ u32x2 paged_transposed(const unsigned short* p) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s4*)p));
 }
+
+// 16 bytes for each lane from base + offset straight to LDS, lane after lane from `to` on (base and `to` are the wave's).  Not the
+// builtin: after that one the compiler has every read of LDS wait for the copy, also those of other buffers.  It does
+// not know of this one: whoever reads waits for vmcnt(0) first (paged_copies_done) and meets the other waves at a barrier.
+__device__ __forceinline__ void paged_copy(const void* base, uint32_t offset, unsigned short* to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               : : "s"((uint32_t)(uintptr_t)(LDS_AS unsigned short*)to), "v"(offset), "s"(base) : "memory");   // (m0 is nobody else's: the compiler sets it where it needs it)
+}
+__device__ __forceinline__ void paged_copies_done() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
 
 // Is the element in the low half an infinity or NaN?
 template <int DT> __device__ __forceinline__ bool paged_odd(uint32_t x) {
@@ -495,7 +505,11 @@ template <int DT> __device__ __forceinline__ uint32_t paged_finite(uint32_t x) {
 template <int D, int BITS, int DT, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAsk a) {
   constexpr int rb = paged_row<D, BITS>(), sb = paged_srow<D, BITS>(), COLS = 32 * WAVES, T = PAGED_TILE, N = WAVES * 64;
-  constexpr int PK = D + 8, PV = D + 32;                    // 16-bit elements between two tokens: reads of 32 keys / of 4 values' parts spread over the banks
+  // 16-bit elements between two tokens in LDS.  Codes are converted on their way and written with a pitch that spreads reads of
+  // 32 keys' / of 4 values' parts over the banks; 16 bits go there directly, 64 lanes' parts one after the other, so that
+  // the parts of a row change places instead (paged_key_part, paged_value_part).
+  constexpr bool DIRECT = BITS == 16;
+  constexpr int PK = DIRECT ? D : D + 8, PV = DIRECT ? D : D + 32;
   constexpr int VP = rb / 16;                               // 16-byte parts of a row
   constexpr int NS = D / 16, CB = D / 32;
   constexpr float SLACK = 8.f;                              // a maximum may be exceeded by 2^8 before everything is scaled anew
@@ -552,6 +566,11 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
   const bool has = BOTH || wave < 2 * T * VP / 64, val0 = !BOTH && wave >= T * VP / 64;   // (else: this wave's load is of values)
   const int ltok = lane / VP, lpart = lane % VP;
   const int tok0 = (wave * 64 / VP) % T;                    // first token of this wave's first group
+  // where part c of token t's keys / values lies in its row (and which part lies in place c)
+  auto key_part = [&](int t, int c) PAGED_INLINE { return DIRECT ? c ^ (t & (VP - 1)) : c; };
+  auto value_part = [&](int t, int c) PAGED_INLINE { return DIRECT ? c ^ ((D == 128 ? t & 3 : t >> 1 & 1) << 2) : c; };
+  // (direct: the part that belongs where this lane's bytes go; its row is lane / VP more than a multiple of 64 / VP)
+  const uint32_t lkey = DIRECT ? ltok * rb + key_part(tok0 + ltok, lpart) * 16 : 0, lvalue = DIRECT ? ltok * rb + value_part(tok0 + ltok, lpart) * 16 : 0;
   const uint32_t lcode = lane * 16 % (16 * rb), lscale = (ltok & 15) * sb + lpart * (128 / BITS) / 32;   // (of a sixteen of tokens)
   u32x4 x[R];
   uint32_t xs[R];
@@ -563,7 +582,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
 #pragma unroll
       for (int i = 0; i < NP; ++i) page[r][i] = table[min((t + tok0 + r * (N / VP) + 16 * i) >> v.page_shift, last_page)];
   };
-  auto load = [&](int t) PAGED_INLINE {
+  auto load = [&](int t, int kb, int vb) PAGED_INLINE {     // (direct: into these buffers)
     gone = false;
     if (!has) return;
 #pragma unroll
@@ -587,7 +606,9 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
           c = lane < 32 ? c : at[1];
           e = lane < 32 ? e : sat[1];
         }
-        x[r + w * G] = *(const u32x4*)(c + ((w * rb) << v.page_shift) + lcode);
+        if constexpr (DIRECT) {
+          paged_copy(c + ((w * rb) << v.page_shift), w ? lvalue : lkey, (w ? lv[vb] : lk[kb]) + (tok0 + r * (N / VP)) * D);
+        } else x[r + w * G] = *(const u32x4*)(c + ((w * rb) << v.page_shift) + lcode);
         if constexpr (BITS < 16) xs[r + w * G] = e[((w * sb) << v.page_shift) + lscale];
       }
     }
@@ -597,15 +618,18 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
   auto stage = [&](int t, int kb, int vb) PAGED_INLINE {
     if (!has) return;
     const bool plain = t >= wg_lo && t + T <= wg_hi && !gone;
+    if constexpr (DIRECT) paged_copies_done();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const bool val = BOTH ? r >= G : val0;
       const int tok = tok0 + (r % G) * (N / VP) + ltok;
+      u32x4* d = (u32x4*)((val ? lv[vb] + tok * PV : lk[kb] + tok * PK) + lpart * (128 / BITS));
       if (__builtin_expect(!plain, 0)) {
         // values that no row of the tile sees, or of no page, count as zeros; keys of no page as NaN
         const int pg = NP > 1 && lane >= 32 ? was[r % G][NP - 1] : was[r % G][0];
         const bool ok = (unsigned)pg < (unsigned)v.n_pages, seen = ok && t + tok < all_hi && t + tok >= all_lo;
         const u32x4 z = {0, 0, 0, 0}, none = {~0u, ~0u, ~0u, ~0u};
+        if constexpr (DIRECT) x[r] = *d;
         if (val) x[r] = seen ? x[r] : z;
         else if (BITS == 16) x[r] = ok ? x[r] : none;
         bool odd = false;
@@ -617,10 +641,9 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
           for (int e = 0; e < 4; ++e) odd |= paged_odd<DT>(x[r][e]) || paged_odd<DT>(x[r][e] >> 16);
         }
         if (val && odd) odd_tile[vb] = t;
+        if constexpr (DIRECT) *d = x[r];
       }
-      u32x4* d = (u32x4*)((val ? lv[vb] + tok * PV : lk[kb] + tok * PK) + lpart * (128 / BITS));
-      if constexpr (BITS == 16) d[0] = x[r];
-      else {
+      if constexpr (!DIRECT) {
 #pragma unroll
         for (int e = 0; e < 16 / BITS; ++e) {
           const u32x2 w = {x[r][BITS == 8 ? 2 * e : e], BITS == 8 ? x[r][2 * e + 1] : 0};
@@ -634,7 +657,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
   auto scores = [&](const unsigned short* kb, f16v& sc) PAGED_INLINE {
     sc = f16v{};
 #pragma unroll
-    for (int j = 0; j < NS; ++j) sc = paged_mfma32<DT>(*(const u32x4*)(kb + n * PK + 16 * j + 8 * h), q[j], sc);
+    for (int j = 0; j < NS; ++j) sc = paged_mfma32<DT>(*(const u32x4*)(kb + n * PK + key_part(n, 2 * j + h) * 8), q[j], sc);
   };
   // O^T += V^T P^T over 32 tokens from t on.  Lane 16 (2 h + i) + j gives the address of token 4 h + j / 4 (and 8 more), channels
   // 16 i + 4 (j % 4) ..
@@ -655,17 +678,19 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
         for (int k = 0; k < CB; ++k)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const uint32_t bits = vb[tok * PV + 32 * k + 8 * (e >> 2) + 4 * h + (e & 3)];
+            const uint32_t bits = vb[tok * PV + value_part(tok, 4 * k + (e >> 2)) * 8 + 4 * h + (e & 3)];
             if (sees && paged_odd<DT>(bits)) o[k][e] += pf * paged_lo<DT>(bits);
           }
       }
     }
-    const unsigned short* from = vb + (4 * h + ((lane & 15) >> 2)) * PV + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    const int row = 4 * h + ((lane & 15) >> 2);
+    const unsigned short* from = vb + row * PV + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int k = 0; k < CB; ++k) {
-        const u32x2 a0 = paged_transposed(from + 16 * j * PV + 32 * k), a1 = paged_transposed(from + (16 * j + 8) * PV + 32 * k);
+        const unsigned short* at = from + 16 * j * PV + (DIRECT ? value_part(row, 4 * k) * 8 : 32 * k);
+        const u32x2 a0 = paged_transposed(at), a1 = paged_transposed(at + 8 * PV);
         u32x4 vv = {a0[0], a0[1], a1[0], a1[1]};
         if constexpr (decltype(fix)::value) {
 #pragma unroll
@@ -691,10 +716,11 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
     float own;
     const float other = paged_other(top, own);
     top = fmaxf(own, other) * scale2;
-    const bool up = top > m + SLACK || (m == -INFINITY && top > m);
+    const bool up = top > fmaxf(m + SLACK, -FLT_MAX);       // (after none, any score is a new maximum)
     const float m2 = up ? top : m, f = up ? paged_exp2(m - m2) : 1.f;
     const float ref = paged_chunk_bias<DT>() - (m2 == -INFINITY ? 0.f : m2);
     m = m2;
+    __builtin_amdgcn_s_setprio(1);                          // (the other wave of the SIMD has its arithmetic meanwhile)
     scores(kb, next);
     float sum = 0;
 #pragma unroll
@@ -710,6 +736,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
         else values(std::false_type{}, vb, before, tb);
       }
     } else values(std::false_type{}, vb, before, tb);
+    __builtin_amdgcn_s_setprio(0);
     asm volatile("" : "+v"(p[0]), "+v"(p[1]), "+v"(sum));   // (before the branch, beside the products, not where they are needed)
     if (__any(up)) {
       l *= f;
@@ -732,11 +759,11 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
   if (tiles > 0) {
     int t0 = tile_at(0), t1 = tile_at(1), t2 = tile_at(2), before = 0;   // tiles i, i + 1, i + 2 (where there are such), i - 1
     pages(t0);
-    load(t0);
+    load(t0, 0, 0);
     pages(t1);
     stage(t0, 0, 0);
     if (tiles > 1) {
-      load(t1);
+      load(t1, 1, 1);
       pages(t2);
       stage(t1, 1, 1);
     }
@@ -749,14 +776,14 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
         const int t3 = M ? tile_at(i + 3) : t2 + T;         // (M: the next may be elsewhere)
         const bool more = i + 2 < tiles;
         if (more) {
-          load(t2);
+          load(t2, k2, (i + 2) & 3);
           pages(t3);
         }
         // (the keys of a tile that is not there give scores that nothing looks at)
         const bool ob = M && odd_tile[(i - 1) & 3] == before, oc = M && odd_tile[i & 3] == t0;
         step(masked, s0, s1, lk[k0] + 32 * PK, p0, p1, M && !i ? nullptr : lv[(i - 1) & 3] + 32 * PV, t0, before + 32, ob);
+        if (more) stage(t2, k2, (i + 2) & 3);               // (nobody reads those buffers)
         step(masked, s1, s0, lk[k1], p1, p0, lv[i & 3], t0 + 32, t0, oc);
-        if (more) stage(t2, k2, (i + 2) & 3);
         __syncthreads();
         const int k = k0;
         k0 = k1;
