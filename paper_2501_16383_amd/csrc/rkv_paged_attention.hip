@@ -870,15 +870,17 @@ __global__ __launch_bounds__(256) void k_paged_chunk_merge(PagedView v, PagedAsk
 // ---- host side ---------------------------------------------------------------------------------
 
 #define RKV_PAGED_CUS 256             // compute units that a launch should fill
-#define RKV_PAGED_FEW 32              // columns (rows times rep) of a sequence that k_paged_few takes
+#define RKV_PAGED_FEW 32              // columns (rows times rep) of a sequence that k_paged_few takes ...
+#define RKV_PAGED_FEW_MIXED 16        // ... where others go to k_paged_chunk: single tokens, half the registers
 #define RKV_PAGED_SPLITS 256          // most splits of a sequence
 #define RKV_PAGED_COLS 256            // columns of a workgroup of k_paged_chunk
 
 // Splits of sequences of max_len tokens whose work units (`units` of them) should become `want`: a multiple of `step` tokens each.
-static void paged_cut(const PagedView& v, int window, int tile, int64_t units, int64_t want, int step, int rows, PagedSplit* sp) {
+// One span of up to `whole` tokens is not cut: the launch that joins splits takes longer than what they save.
+static void paged_cut(const PagedView& v, int window, int tile, int64_t units, int64_t want, int step, int whole, int rows, PagedSplit* sp) {
   int64_t span = v.max_len;
   if (window && span > (int64_t)window + rows + tile - 1) span = (int64_t)window + rows + tile - 1;
-  int64_t n = (want + units - 1) / units;
+  int64_t n = span <= whole ? 1 : (want + units - 1) / units;
   if (n > RKV_PAGED_SPLITS) n = RKV_PAGED_SPLITS;
   const int64_t c = ((span + n - 1) / n + step - 1) / step * step;
   sp->chunk = (int)c;
@@ -886,43 +888,45 @@ static void paged_cut(const PagedView& v, int window, int tile, int64_t units, i
 }
 // Bytes of partial results, for any window (a shorter span may be cut into more splits than a longer one, but never into
 // more than are wanted)
-static size_t paged_cut_bytes(const PagedView& v, int64_t units, int64_t want, int step, int cols, int D) {
+static size_t paged_cut_bytes(const PagedView& v, int64_t units, int64_t want, int step, int whole, int cols, int D) {
+  if (v.max_len <= whole) return 0;
   int64_t n = (want + units - 1) / units, cut = ((int64_t)v.max_len + step - 1) / step;
   if (n > RKV_PAGED_SPLITS) n = RKV_PAGED_SPLITS;
   if (n > cut) n = cut;
   return n > 1 ? (size_t)units * cols * n * (D + 2) * 4 : 0;
 }
 
+static bool has_chunk(const PagedView& v) { return (int64_t)v.max_new * v.rep > RKV_PAGED_FEW; }
+static bool has_few(const PagedView& v) { return v.n_seqs > 1 || !has_chunk(v); }
+
 // k_paged_few: a unit is a (sequence, KV head); splits of at least 128 tokens (32 for each wave).  Two workgroups for each
 // compute unit have enough bytes in flight, and four where a row is 64 bytes or less (32768 tokens, 32 heads, 4 bits: 31.0 us with
 // four, 36.6 with two; 8 x 4096 tokens, 8 heads, 8 bits: 20.5 with two, 24.5 with four).
 static int64_t few_units(const PagedView& v) { return (int64_t)v.n_seqs * v.Hkv; }
-static int few_cols(const PagedView& v) { return (int64_t)v.max_new * v.rep <= 16 ? 16 : 32; }
+static int few_cols(const PagedView& v) { return (int64_t)v.max_new * v.rep <= 16 || has_chunk(v) ? 16 : 32; }
 static int64_t few_want(int D, int bits) { return (D * bits <= 512 ? 4 : 2) * RKV_PAGED_CUS; }
 #define FEW_STEP 128
+#define FEW_WHOLE 512
 // k_paged_chunk: a unit is a tile of columns and a KV head; a workgroup for each compute unit, splits of at least 512 tokens
 static int64_t chunk_units(const PagedView& v) {
-  // every sequence may have a tile that is not full
-  const int64_t cols = (int64_t)v.n_rows * v.rep, seqs = v.n_seqs < cols / RKV_PAGED_FEW ? v.n_seqs : cols / RKV_PAGED_FEW;
+  // every sequence of more than RKV_PAGED_FEW_MIXED columns may have a tile that is not full (one alone has any number)
+  const int64_t cols = (int64_t)v.n_rows * v.rep, most = cols / RKV_PAGED_FEW_MIXED, seqs = v.n_seqs < most ? v.n_seqs : most;
   return (cols / RKV_PAGED_COLS + seqs) * v.Hkv;
 }
 #define CHUNK_WANT RKV_PAGED_CUS
 #define CHUNK_STEP 512
-static bool has_few(const PagedView& v) { return v.n_seqs > 1 || (int64_t)v.max_new * v.rep <= RKV_PAGED_FEW; }
-static bool has_chunk(const PagedView& v) { return (int64_t)v.max_new * v.rep > RKV_PAGED_FEW; }
-
 // work space: k_paged_few's partial results, then k_paged_chunk's
 static size_t few_bytes(const PagedView& v, int D, int bits) {
-  const size_t n = has_few(v) ? paged_cut_bytes(v, few_units(v), few_want(D, bits), FEW_STEP, few_cols(v), D) : 0;
+  const size_t n = has_few(v) ? paged_cut_bytes(v, few_units(v), few_want(D, bits), FEW_STEP, FEW_WHOLE, few_cols(v), D) : 0;
   return (n + 255) & ~(size_t)255;
 }
 size_t rkv_paged_attention_scratch(const PagedView& v, int D, int bits) {
-  return few_bytes(v, D, bits) + (has_chunk(v) ? paged_cut_bytes(v, chunk_units(v), CHUNK_WANT, CHUNK_STEP, RKV_PAGED_COLS, D) : 0);
+  return few_bytes(v, D, bits) + (has_chunk(v) ? paged_cut_bytes(v, chunk_units(v), CHUNK_WANT, CHUNK_STEP, CHUNK_STEP, RKV_PAGED_COLS, D) : 0);
 }
 
 template <int D, int BITS, int DT, int NB>
 static void launch_few(const PagedView& v, PagedAsk a, void* scratch, hipStream_t s) {
-  paged_cut(v, a.window, 32, few_units(v), few_want(D, BITS), FEW_STEP, RKV_PAGED_FEW, &a.sp);
+  paged_cut(v, a.window, 32, few_units(v), few_want(D, BITS), FEW_STEP, FEW_WHOLE, RKV_PAGED_FEW, &a.sp);
   a.sp.acc = (float*)scratch;
   a.sp.ml = (float2*)(a.sp.acc + few_units(v) * (16 * NB) * a.sp.splits * D);
   k_paged_few<D, BITS, DT, NB><<<dim3(a.sp.splits, v.Hkv, v.n_seqs), 256, 0, s>>>(v, a);
@@ -931,8 +935,8 @@ static void launch_few(const PagedView& v, PagedAsk a, void* scratch, hipStream_
 
 template <int D, int BITS, int DT>
 static void launch(const PagedView& v, PagedAsk a, void* scratch, hipStream_t s) {
-  a.few = RKV_PAGED_FEW;
   a.mixed = has_chunk(v);
+  a.few = a.mixed ? RKV_PAGED_FEW_MIXED : RKV_PAGED_FEW;
   if (has_few(v)) {
     if (few_cols(v) == 16) launch_few<D, BITS, DT, 1>(v, a, scratch, s);
     else launch_few<D, BITS, DT, 2>(v, a, scratch, s);
@@ -942,7 +946,7 @@ static void launch(const PagedView& v, PagedAsk a, void* scratch, hipStream_t s)
     const int64_t units = chunk_units(v);
     // (rows of a unit; without `causal` its first row sees all behind it)
     const int rows = a.causal && v.max_new > RKV_PAGED_COLS ? RKV_PAGED_COLS : v.max_new;
-    paged_cut(v, a.window, PAGED_TILE, units, CHUNK_WANT, CHUNK_STEP, rows, &a.sp);
+    paged_cut(v, a.window, PAGED_TILE, units, CHUNK_WANT, CHUNK_STEP, CHUNK_STEP, rows, &a.sp);
     a.sp.acc = (float*)((char*)scratch + few_bytes(v, D, BITS));
     a.sp.ml = (float2*)(a.sp.acc + units * RKV_PAGED_COLS * a.sp.splits * D);
     k_paged_chunk<D, BITS, DT, 8><<<dim3((unsigned)units, a.sp.splits), 512, 0, s>>>(v, a);
