@@ -64,7 +64,7 @@ def attention(q: np.ndarray, k: np.ndarray, v: np.ndarray, first: int, causal=Tr
     scale = D**-0.5 if scale is None else scale
     p = np.arange(first, first + n)[:, None]
     t = np.arange(L)[None]
-    sees = np.ones((n, L), bool)
+    sees = np.repeat(p >= 0, L, axis=1)                        # a row in front of the first token sees nothing
     if causal:
         sees &= t <= p
     if window:

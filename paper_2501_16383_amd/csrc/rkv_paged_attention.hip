@@ -4,7 +4,7 @@
 // read one KV head - its new tokens times the rep query heads - are the columns of two matrix products,
 //   S^T[token][column] = K . Q^T          O^T[channel][column] = V^T . P^T,
 // so that a lane of the result owns one column: the running maximum and sum of its softmax are plain registers, and
-// the four (eight) weights a lane gets from the first product are, in their order, an operand of the second.
+// the weights a lane gets from the first product are, in their order, an operand of the second.
 // (Which token is which index of the sum is free as long as both operands agree.)  Weights are powers of two of
 // scores in fp32; the sum of weights is taken in fp32 from unrounded weights.
 #include <cfloat>
@@ -104,13 +104,12 @@ struct PagedAsk {
   PagedSplit sp;
 };
 
-// A column's result: out and lse, or the partial result of a split
 template <int DT> __device__ __forceinline__ float paged_lse(float m, float sum) {
   return sum == 0 ? -INFINITY : (m + __log2f(sum) - paged_bias<DT>()) * 0.69314718055994531f;
 }
 
-// Tokens that the row at position p sees: lo .. hi - 1
-__device__ __forceinline__ int paged_hi_of(const PagedAsk& a, const PagedSeq& s, int p) { return a.causal ? min(max(p + 1, 0), s.len) : s.len; }
+// Tokens that the row at position p sees: lo .. hi - 1 (none in front of the first token)
+__device__ __forceinline__ int paged_hi_of(const PagedAsk& a, const PagedSeq& s, int p) { return p < 0 ? 0 : a.causal ? min(p + 1, s.len) : s.len; }
 __device__ __forceinline__ int paged_lo_of(const PagedAsk& a, int p) { return a.window ? max(0, p - a.window + 1) : 0; }
 
 // NaN for every row of a bad sequence that reads this KV head
@@ -463,8 +462,14 @@ __global__ __launch_bounds__(256) void k_paged_merge(PagedView v, PagedAsk a) {
 // ---- many rows: chunks, prompts ----------------------------------------------------------------
 //
 // A workgroup takes 32 WAVES columns of one (sequence, KV head), 32 a wave, and walks the tokens that they see in
-// tiles of 64.  Tiles are converted to 16 bits as they are staged in LDS, two of them: the next one's bytes come from
-// memory while one is computed, with one barrier a tile.
+// tiles of 64, which it stages in LDS as 16-bit rows: tile i + 2 comes from memory while tile i is computed, with one
+// barrier a tile.  A wave works in half tiles: the softmax of one stands beside the scores of the next and the values of the one
+// before, so that matrix and vector unit have work that does not wait for the other.
+//
+// What bounds it: every product of 32 x 32 x 16 reads 1 KiB of LDS for 32 columns, and a compute unit's four matrix units
+// ask for those 128 bytes a cycle that its LDS gives.  8192 tokens, 32 query heads on 8 KV heads of 128, 16 bits: the products
+// and their reads alone take 390 us, the softmax alone 250, staging adds 80; together 530-560 us (1.0 PFLOP/s).  64 columns a
+// wave would halve the reads, but their 512 registers leave one wave a SIMD, which took twice as long.
 #define PAGED_TILE 64
 
 // The tile of columns that a workgroup takes: sequence and first column, or b = n_seqs.  Sequences of more than `few`

@@ -7,6 +7,13 @@ from dataclasses import dataclass, replace
 from .binding import _check, _CPagedBatch, _CPagedConfig, _dev, _device, _stream, load_library
 
 
+def _int32(**values):
+    """Whole numbers that the library's 32-bit fields hold (ctypes would cut others off)."""
+    for name, x in values.items():
+        if not isinstance(x, int) or not -(2**31) <= x < 2**31:
+            raise ValueError(f"{name} must be an int of 32 bits, not {x!r}")
+
+
 @dataclass
 class RkvPagedConfig:
     """rkv_paged_config: bits 16, 8 (E4M3 codes) or 4 (E2M1 codes); dtype 0 fp16, 1 bf16."""
@@ -19,6 +26,7 @@ class RkvPagedConfig:
     dtype: int = 0
 
     def to_c(self) -> _CPagedConfig:
+        _int32(**vars(self))
         return _CPagedConfig(self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_tokens, self.n_pages, self.bits, self.dtype)
 
 
@@ -36,7 +44,7 @@ class RkvPagedBatch:
     call anew (and by every replay of a captured one); n_rows, max_new and max_len are the host's bounds on them (n_rows
     and the tables' capacity where not given).  The object is fixed: a batch of other bounds or tensors is another object."""
 
-    __slots__ = ("page_table", "row_start", "lengths", "device", "n_rows", "_c")
+    __slots__ = ("page_table", "row_start", "lengths", "device", "n_rows", "_c", "_defaults")
 
     def __init__(self, page_table, row_start, lengths, n_rows: int, max_new: int = None, max_len: int = None):
         import torch
@@ -51,13 +59,15 @@ class RkvPagedBatch:
         self.page_table, self.row_start, self.lengths = page_table, row_start, lengths
         self.device, self.n_rows = page_table.device, n_rows
         n_seqs, max_pages = page_table.shape
-        self._c = _CPagedBatch(page_table.data_ptr(), row_start.data_ptr(), lengths.data_ptr(), n_seqs, max_pages, n_rows,
-                               n_rows if max_new is None else max_new, -1 if max_len is None else max_len)
+        max_new = n_rows if max_new is None else max_new
+        _int32(n_rows=n_rows, max_new=max_new, max_len=0 if max_len is None else max_len, n_seqs=n_seqs, max_pages=max_pages)
+        self._defaults = max_len is None
+        self._c = _CPagedBatch(page_table.data_ptr(), row_start.data_ptr(), lengths.data_ptr(), n_seqs, max_pages, n_rows, max_new, max_len or 0)
 
     def to_c(self, cfg: RkvPagedConfig) -> _CPagedBatch:
         """The C structure, for a cache of this configuration."""
         c = self._c
-        if c.max_len != -1:
+        if not self._defaults:
             return c
         return _CPagedBatch(c.dev_page_table, c.dev_row_start, c.dev_lengths, c.n_seqs, c.max_pages, c.n_rows, c.max_new,
                             min(c.max_pages * cfg.page_tokens, 1 << 30))
@@ -143,6 +153,8 @@ class RkvPagedCache:
             lse = torch.empty((n, cfg.n_q_heads), dtype=torch.float32, device=dev) if want_lse else None
         elif _dev(lse, torch.float32, "lse").shape != (n, cfg.n_q_heads) or lse.device != dev:
             raise ValueError("lse must be [n_rows, n_q_heads]")
+        if not 0 <= window < 2**31:
+            raise ValueError("window must be an int of 32 bits, 0 for none")
         cb, need = self._batch(batch), C.c_size_t()
         rc = self.lib.rkv_paged_scratch(self._at, cb, C.byref(need))
         if rc:

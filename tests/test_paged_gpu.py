@@ -254,6 +254,53 @@ def test_long_sequences(bits, dtype, D, new):
     run(Setup(lens, hq=2, hkv=1, D=D, bits=bits, dtype=dtype, page=64, seed=new), lens, news)
 
 
+@pytest.mark.parametrize("bits,D", [(16, 128), (8, 64), (4, 128)])
+@pytest.mark.parametrize("news", [[4, 1, 2, 4], [5, 8, 1, 7], [9, 5, 4, 1], [64, 8, 4, 1], [65, 7, 1, 128]], ids=str)
+def test_columns_around_the_kernels_bounds(bits, D, news):
+    """16, 32, 36, 256 and 260 columns of a KV head and few beside them, over enough tokens to be cut into splits."""
+    run(Setup([1400, 900, 700, 333], hq=4, hkv=1, D=D, bits=bits, dtype="bf16", page=16, seed=sum(news)), [1400, 900, 700, 333], news)
+
+
+@pytest.mark.parametrize("window", [0, 50, 700])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("new", [1, 3, 90, 300])
+def test_tables_far_wider_than_the_sequences(window, causal, new):
+    """Without max_len the host cuts the table's capacity into splits: of these sequences most are empty."""
+    s = Setup([600, 310], hq=2, hkv=1, seed=new)
+    s.dtable = torch.cat([s.dtable, torch.full((2, 4000), 2**30, dtype=torch.int32, device=DEV)], 1)
+    run(s, [600, 310], [new, 1], causal=causal, window=window)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_more_rows_than_tokens(causal):
+    """Rows in front of the first token see nothing, whatever the direction."""
+    out, lse, _ = run(Setup([40, 3, 0], hq=4, hkv=2, seed=3), [40, 3, 0], [100, 5, 7], causal=causal)
+    assert (out[:60] == 0).all() and (lse[:60] == -np.inf).all() and (out[60:100] != 0).any() and (lse[105:] == -np.inf).all()
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+def test_a_page_outside_the_pool_in_a_long_sequence(bits):
+    """Splits whose pages are in order, and one whose are not, meet."""
+    lens, news = [3000, 2000], [40, 1]
+    s = Setup(lens, hq=4, hkv=2, bits=bits, page=32, seed=6)
+    out0, _, q = run(s, lens, news)
+    s.dtable[1, 20] = s.n_pages
+    out = s.cache.attention(q, s.batch(lens, news))
+    assert torch.equal(out[:40], out0[:40]) and torch.isnan(out[40]).all()
+    s.dtable[0, 92] = -1                                       # tokens 2944 .. 2975: rows 0 ..: every row but those before 2944
+    assert torch.isnan(s.cache.attention(q, s.batch(lens, news))).all()
+    s.dtable[0, 92], s.dtable[0, 93] = s.table[0, 92], -1      # tokens 2976 ..: from row 16 on
+    out = s.cache.attention(q, s.batch(lens, news))
+    assert torch.equal(out[:16], out0[:16]) and torch.isnan(out[16:40]).all()
+
+
+def test_output_in_the_queries_place():
+    lens, news = [700, 300], [90, 2]
+    s = Setup(lens, hq=4, hkv=2, seed=5)
+    out0, _, q = run(s, lens, news)
+    assert s.cache.attention(q, s.batch(lens, news), out=q) is q and torch.equal(q, out0)
+
+
 def test_many_sequences():
     lens = [(7 * i) % 50 for i in range(300)]
     news = [min(n, 1 + (i % 3 == 0) * (i % 20)) for i, n in enumerate(lens)]
@@ -525,19 +572,22 @@ def test_refusals_of_the_binding():
         s.cache.append(x[:1].expand(8, 2, 128), x, b)
     with pytest.raises(R.RkvError):                            # not aligned
         s.cache.append(torch.zeros(8 * 256 + 1, dtype=torch.float16, device=DEV)[1:].view(8, 2, 128), x, b)
-    for kw in (dict(window=-1), dict(scale=float("nan"))):
+    for kw in (dict(scale=float("nan")), dict(scale=1e300)):
         with pytest.raises(R.RkvError):
             s.cache.attention(q, b, **kw)
     for kw in (dict(out=q.float()), dict(lse=q)):
         with pytest.raises(TypeError):
             s.cache.attention(q, b, **kw)
-    for kw in (dict(out=q[:4]), dict(lse=torch.zeros(8, 2, device=DEV))):
+    for kw in (dict(out=q[:4]), dict(lse=torch.zeros(8, 2, device=DEV)), dict(window=-1), dict(window=2**32)):
         with pytest.raises(ValueError):
             s.cache.attention(q, b, **kw)
     with pytest.raises(ValueError):
         R.RkvPagedCache(s.cfg, device=DEV, mem=torch.zeros(100, dtype=torch.uint8, device=DEV))
     with pytest.raises(ValueError):
         R.RkvPagedBatch(s.dtable, ints([0, 1, 2]), ints([40]), 2)
+    for kw in (dict(n_rows=2**32 + 8), dict(n_rows=8, max_new=2**32 + 8), dict(n_rows=8, max_len=2**32 + 40)):   # (cut to 32 bits they would do)
+        with pytest.raises(ValueError):
+            R.RkvPagedBatch(s.dtable, ints([0, 8]), ints([40]), **kw)
     with pytest.raises(R.RkvError):
         s.cache.attention(q, R.RkvPagedBatch(s.dtable, ints([0, 8]), ints([40]), 8, max_len=10**6))
     # too little work space is refused by the library, before anything runs
