@@ -130,6 +130,9 @@ template <int D, int DT> __device__ __forceinline__ void paged_bad_rows(const Pa
 // (lane l: token l % 16, a quarter of its channels); values, whose operand runs along the tokens, pass through
 // the wave's own LDS as 16-bit rows and come back transposed.  The next tile's values are asked for as soon as
 // these are in LDS, its keys as soon as these are multiplied.
+//
+// What bounds it: the stream of the cache.  32 sequences of 8192 tokens, 8 KV heads of 128, 8 bits: 96 us = 5.8 TB/s, and 94
+// with the arithmetic left out; more bytes in flight (three or four workgroups a compute unit) change nothing.
 template <int D, int BITS, int DT, int NB>
 __global__ __launch_bounds__(256, NB == 1 ? 3 : 2) void k_paged_few(PagedView v, PagedAsk a) {
   constexpr int KL = D * BITS / 8 / 4 / 16;                 // 16-byte loads of a quarter row of keys (0: one of 8 bytes)
@@ -142,7 +145,7 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 2) void k_paged_few(PagedView v,
   __shared__ float meet[2][4][16];
   static_assert(4 * 16 * OP * 4 <= 4 * 32 * PITCH * 2, "the waves' results fit the values' rows");
 
-  const int split = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
+  const int kvh = blockIdx.x, split = blockIdx.y, b = blockIdx.z;   // (the heads of a page at the same time)
   const PagedSeq s = paged_seq(v, b);
   const int rows = s.last - s.first, cols = rows * v.rep;
   if (rows == 0) return;
@@ -266,10 +269,6 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 2) void k_paged_few(PagedView v,
       u32x4* d = (u32x4*)(vl + tok * PITCH + part * (128 / BITS));
       if constexpr (BITS == 16) {
         d[0] = vx[r];
-        if (mixed_rows) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) odd |= paged_odd<DT>(vx[r][e]) || paged_odd<DT>(vx[r][e] >> 16);
-        }
       } else {
         const float sc = paged_scale(vs[r]);
         odd |= vs[r] == 255;
@@ -279,6 +278,12 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 2) void k_paged_few(PagedView v,
           d[e] = paged_decode8<DT, BITS>(w, sc);
         }
       }
+    }
+    if (BITS == 16 && mixed_rows) {
+#pragma unroll
+      for (int r = 0; r < VL; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd |= paged_odd<DT>(vx[r][e]) || paged_odd<DT>(vx[r][e] >> 16);
     }
     if (more) {
       pages(t + 128);
@@ -426,7 +431,8 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 2) void k_paged_few(PagedView v,
   }
 }
 
-// One column's splits together, by a wave: u0 is the first one's index, at the column's place in the output.
+// One column's splits together, by a wave: u0 is the first one's index, at the column's place in the output.  A chain of three
+// latencies, 4 us for the largest batches.
 template <int D, int DT> __device__ __forceinline__ void paged_join(const PagedAsk& a, int64_t u0, int n, int64_t at) {
   const int lane = threadIdx.x & 63;
   float mm = -INFINITY;
@@ -512,7 +518,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
   constexpr int rb = paged_row<D, BITS>(), sb = paged_srow<D, BITS>(), COLS = 32 * WAVES, T = PAGED_TILE, N = WAVES * 64;
   // 16-bit elements between two tokens in LDS.  Codes are converted on their way and written with a pitch that spreads reads of
   // 32 keys' / of 4 values' parts over the banks; 16 bits go there directly, 64 lanes' parts one after the other, so that
-  // the parts of a row change places instead (paged_key_part, paged_value_part).
+  // the parts of a row change places instead (key_part, value_part).
   constexpr bool DIRECT = BITS == 16;
   constexpr int PK = DIRECT ? D : D + 8, PV = DIRECT ? D : D + 32;
   constexpr int VP = rb / 16;                               // 16-byte parts of a row
@@ -934,7 +940,7 @@ static void launch_few(const PagedView& v, PagedAsk a, void* scratch, hipStream_
   paged_cut(v, a.window, 32, few_units(v), few_want(D, BITS), FEW_STEP, FEW_WHOLE, RKV_PAGED_FEW, &a.sp);
   a.sp.acc = (float*)scratch;
   a.sp.ml = (float2*)(a.sp.acc + few_units(v) * (16 * NB) * a.sp.splits * D);
-  k_paged_few<D, BITS, DT, NB><<<dim3(a.sp.splits, v.Hkv, v.n_seqs), 256, 0, s>>>(v, a);
+  k_paged_few<D, BITS, DT, NB><<<dim3(v.Hkv, a.sp.splits, v.n_seqs), 256, 0, s>>>(v, a);
   if (a.sp.splits > 1) k_paged_merge<D, DT, NB><<<dim3(4 * NB, v.Hkv, v.n_seqs), 256, 0, s>>>(v, a);
 }
 
