@@ -388,7 +388,7 @@ int rkv_paged_scratch(const rkv_paged_config* cfg, const rkv_paged_batch* batch,
  * of prompts, drafted tokens, single tokens, in any mixture.  The row at position p sees the tokens t of its
  * sequence with t <= p (all of them without `causal`) and, with window > 0, t > p - window.
  *   dev_q      [n_rows][n_q_heads][head_dim] of the cache's type, rows q_stride elements apart (as k_stride)
- *   scale      of the scores, finite (1 / sqrt(head_dim) by custom)
+ *   scale      of the scores, finite, also times log2(e) (1 / sqrt(head_dim) by custom)
  *   dev_out    [n_rows][n_q_heads][head_dim] of the cache's type, dense
  *   dev_lse    [n_rows][n_q_heads] fp32 log-sum-exp of the scaled scores, or NULL
  *   dev_scratch  256-byte aligned, scratch_bytes >= what rkv_paged_scratch says for this batch (else

@@ -311,7 +311,7 @@ RKV_EXPORT int rkv_paged_attention(const rkv_paged_config* cfg, const void* dev_
   PagedView v{};
   const int rc = check_batch(cfg, batch, (void*)dev_pool, &v);
   if (rc != RKV_OK) return rc;
-  if ((causal != 0 && causal != 1) || window < 0 || !__builtin_isfinite(scale)) return RKV_EINVAL;
+  if ((causal != 0 && causal != 1) || window < 0 || !__builtin_isfinite(scale * 1.4426950408889634f)) return RKV_EINVAL;
   if (v.n_rows == 0) return RKV_OK;
   if (!dev_pool || !rows_ok(cfg, dev_q, q_stride, cfg->n_q_heads) || !dev_out || ((uintptr_t)dev_out & 15) || ((uintptr_t)dev_lse & 3)) return RKV_EINVAL;
   const size_t need = rkv_paged_attention_scratch(v, cfg->head_dim, cfg->bits);

@@ -431,26 +431,41 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 2) void k_paged_few(PagedView v,
   }
 }
 
-// One column's splits together, by a wave: u0 is the first one's index, at the column's place in the output.  A chain of three
-// latencies, 4 us for the largest batches.
+// One column's splits together, by a wave: u0 is the first one's index, `at` the column's place in the output.  Eight at a time are
+// asked for together, maxima and all, so that a chain of latencies is what it takes: 4 us for the largest batches.
 template <int D, int DT> __device__ __forceinline__ void paged_join(const PagedAsk& a, int64_t u0, int n, int64_t at) {
+  constexpr int W = 8, C = D / 64;                          // splits at a time; channels of a lane
   const int lane = threadIdx.x & 63;
-  float mm = -INFINITY;
-  for (int i = lane; i < n; i += 64) mm = fmaxf(mm, a.sp.ml[u0 + i].x);
-  for (int o = 32; o; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o));
-  const float ref = mm == -INFINITY ? 0.f : mm;
-  float sum = 0, acc[D / 64] = {};
-#pragma unroll 4
-  for (int i = 0; i < n; ++i) {
-    const float2 ml = a.sp.ml[u0 + i];
-    const float f = paged_exp2(ml.x - ref);
-    sum += f * ml.y;
+  float m = -INFINITY, sum = 0, acc[C] = {};
+  for (int i0 = 0; i0 < n; i0 += W) {
+    float2 ml[W];
+    float x[W][C];
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) acc[j] += f * a.sp.acc[(u0 + i) * D + lane + 64 * j];
+    for (int i = 0; i < W; ++i) {
+      const int64_t u = u0 + min(i0 + i, n - 1);
+      ml[i] = a.sp.ml[u];
+#pragma unroll
+      for (int j = 0; j < C; ++j) x[i][j] = a.sp.acc[u * D + lane + 64 * j];
+    }
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < W; ++i) top = fmaxf(top, ml[i].x);
+    const float ref = top == -INFINITY ? 0.f : top, f0 = paged_exp2(m - ref);
+    sum *= f0;
+#pragma unroll
+    for (int j = 0; j < C; ++j) acc[j] *= f0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const float f = i0 + i < n ? paged_exp2(ml[i].x - ref) : 0.f;
+      sum += f * (i0 + i < n ? ml[i].y : 0.f);              // (not 0 times a NaN)
+#pragma unroll
+      for (int j = 0; j < C; ++j) acc[j] += f * (i0 + i < n ? x[i][j] : 0.f);
+    }
+    m = top;
   }
 #pragma unroll
-  for (int j = 0; j < D / 64; ++j) a.out[at * D + lane + 64 * j] = (unsigned short)paged_pair<DT>(sum == 0 ? 0.f : acc[j] / sum, 0.f);
-  if (a.lse && lane == 0) a.lse[at] = paged_lse<DT>(mm, sum);
+  for (int j = 0; j < C; ++j) a.out[at * D + lane + 64 * j] = (unsigned short)paged_pair<DT>(sum == 0 ? 0.f : acc[j] / sum, 0.f);
+  if (a.lse && lane == 0) a.lse[at] = paged_lse<DT>(m, sum);
 }
 
 template <int D, int DT, int NB>

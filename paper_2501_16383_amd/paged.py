@@ -42,7 +42,7 @@ class RkvPagedBatch:
 
     page_table [n_seqs, max_pages], row_start [n_seqs + 1] and lengths [n_seqs] are int32 tensors on the device, read by every
     call anew (and by every replay of a captured one); n_rows, max_new and max_len are the host's bounds on them (n_rows
-    and the tables' capacity where not given).  The object is fixed: a batch of other bounds or tensors is another object."""
+    and the tables' capacity where not given: close bounds choose the better launch, max_new = 1 for single tokens).  The object is fixed: a batch of other bounds or tensors is another object."""
 
     __slots__ = ("page_table", "row_start", "lengths", "device", "n_rows", "_c", "_defaults")
 

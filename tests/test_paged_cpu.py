@@ -143,7 +143,7 @@ def test_arguments_that_are_refused(lib):
         assert calls(lib, batch=b, ks=stride)[:2] == [E] * 2 and calls(lib, batch=b, vs=stride)[:2] == [E] * 2
     for stride in (4088, 4100, 0, -4096, 1 << 31):
         assert calls(lib, batch=b, qs=stride)[2] == E
-    for kw in (dict(causal=2), dict(window=-1), dict(scale=float("nan")), dict(scale=float("inf")), dict(lse=FAKE + 2)):
+    for kw in (dict(causal=2), dict(window=-1), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=3e38), dict(lse=FAKE + 2)):
         assert calls(lib, batch=b, **kw)[2] == E
 
 
