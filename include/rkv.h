@@ -9,6 +9,8 @@
  *          kept in fp16 (Sec. 4.3);
  *   read   (decoding phase, Eq. 4-5; the online steps of Sec. 4.4 undone):
  *          dequantize, undo reorder and rotation, RoPE, softmax(q.K^T/sqrt(d)).V.
+ * Beside it stands a cache in pages (rkv_paged_*) in 16 bits or floating-point codes of 8 or 4, with
+ * attention of prompts, chunks and single tokens over it.
  *
  * General rules
  *   - Every pointer named dev_* is DEVICE memory owned by the caller; host_* is host memory.

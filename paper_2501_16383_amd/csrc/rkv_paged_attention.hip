@@ -489,8 +489,9 @@ __global__ __launch_bounds__(256) void k_paged_merge(PagedView v, PagedAsk a) {
 //
 // What bounds it: every product of 32 x 32 x 16 reads 1 KiB of LDS for 32 columns, and a compute unit's four matrix units
 // ask for those 128 bytes a cycle that its LDS gives.  8192 tokens, 32 query heads on 8 KV heads of 128, 16 bits: the products
-// and their reads alone take 390 us, the softmax alone 250, staging adds 80; together 530-560 us (1.0 PFLOP/s).  64 columns a
-// wave would halve the reads, but their 512 registers leave one wave a SIMD, which took twice as long.
+// and their reads alone take 390 us, the softmax alone 250, staging adds 80; together 530-560 us (1.0 PFLOP/s), the matrix units
+// half busy at the 1.8 GHz that power allows then.  64 columns a wave would halve the reads, but their 512 registers leave one
+// wave a SIMD, which took twice as long.
 #define PAGED_TILE 64
 
 // The tile of columns that a workgroup takes: sequence and first column, or b = n_seqs.  Sequences of more than `few`
@@ -794,8 +795,22 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
       stage(t1, 1, 1);
     }
     __syncthreads();
-    scores(lk[0], s0);
     int i = 0, k0 = 0, k1 = 1, k2 = 2;                      // buffers of keys of tiles i, i + 1, i + 2
+    // a wave of no columns only stages
+    if (c0 + wave * 32 >= cols) {
+      for (; i < tiles; ++i) {
+        if (i + 2 < tiles) {
+          load(t2, k2, (i + 2) & 3);
+          pages(tile_at(i + 3));
+          stage(t2, k2, (i + 2) & 3);
+        }
+        __syncthreads();
+        t2 = tile_at(i + 3);
+        k2 = k2 == 2 ? 0 : k2 + 1;                          // (the buffer of tile i + 3 is tile i's)
+      }
+      return;
+    }
+    scores(lk[0], s0);
     auto walk = [&](auto masked, int end) PAGED_INLINE {
       constexpr bool M = decltype(masked)::value;
       for (; i < end; ++i) {
@@ -854,7 +869,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
   }
 }
 
-// The splits of k_paged_chunk together: they are few.  A lane takes four channels of a column.
+// The splits of k_paged_chunk together.  A lane takes four channels of a column.
 template <int D, int DT, int COLS>
 __global__ __launch_bounds__(256) void k_paged_chunk_merge(PagedView v, PagedAsk a) {
   const int kvh = blockIdx.x % v.Hkv, unit = blockIdx.x / v.Hkv;
@@ -874,17 +889,33 @@ __global__ __launch_bounds__(256) void k_paged_chunk_merge(PagedView v, PagedAsk
     const int c = (blockIdx.y * 2 + r) * STEP + threadIdx.x / LANES;
     if (c0 + c >= cols) return;
     const int64_t u0 = (((int64_t)unit * v.Hkv + kvh) * COLS + c) * a.sp.splits;
+    constexpr int W = 8;                                    // splits asked for together
     float mm = -INFINITY, sum = 0;
-    for (int i = 0; i < n; ++i) mm = fmaxf(mm, a.sp.ml[u0 + i].x);
-    const float ref = mm == -INFINITY ? 0.f : mm;
     f4 acc = {0, 0, 0, 0};
-    for (int i = 0; i < n; ++i) {
-      const float2 ml = a.sp.ml[u0 + i];
-      const f4 x = *(const f4*)(a.sp.acc + (u0 + i) * D + ch);
-      const float f = paged_exp2(ml.x - ref);
-      sum += f * ml.y;
+    for (int i0 = 0; i0 < n; i0 += W) {
+      float2 ml[W];
+      f4 x[W];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] += f * x[e];
+      for (int i = 0; i < W; ++i) {
+        const int64_t u = u0 + min(i0 + i, n - 1);
+        ml[i] = a.sp.ml[u];
+        x[i] = *(const f4*)(a.sp.acc + u * D + ch);
+      }
+      float top = mm;
+#pragma unroll
+      for (int i = 0; i < W; ++i) top = fmaxf(top, ml[i].x);
+      const float ref = top == -INFINITY ? 0.f : top, f0 = paged_exp2(mm - ref);
+      sum *= f0;
+      acc *= f0;
+#pragma unroll
+      for (int i = 0; i < W; ++i)
+        if (i0 + i < n) {
+          const float f = paged_exp2(ml[i].x - ref);
+          sum += f * ml[i].y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[e] += f * x[i][e];
+        }
+      mm = top;
     }
     const int64_t at = (int64_t)(s.first + (c0 + c) / v.rep) * v.Hq + kvh * v.rep + (c0 + c) % v.rep;
     const float inv = sum == 0 ? 0.f : 1.f / sum;
@@ -935,7 +966,7 @@ static int64_t few_want(int D, int bits) { return (D * bits <= 512 ? 4 : 2) * RK
 #define FEW_WHOLE 512
 // k_paged_chunk: a unit is a tile of columns and a KV head; a workgroup for each compute unit, splits of at least 512 tokens
 static int64_t chunk_units(const PagedView& v) {
-  // every sequence of more than RKV_PAGED_FEW_MIXED columns may have a tile that is not full (one alone has any number)
+  // every sequence of more than RKV_PAGED_FEW_MIXED columns, and one alone, may have a tile that is not full
   const int64_t cols = (int64_t)v.n_rows * v.rep, most = cols / RKV_PAGED_FEW_MIXED, seqs = v.n_seqs < most ? v.n_seqs : most;
   return (cols / RKV_PAGED_COLS + seqs) * v.Hkv;
 }
