@@ -490,8 +490,7 @@ __global__ __launch_bounds__(256) void k_paged_merge(PagedView v, PagedAsk a) {
 // What bounds it: every product of 32 x 32 x 16 reads 1 KiB of LDS for 32 columns, and a compute unit's four matrix units
 // ask for those 128 bytes a cycle that its LDS gives.  8192 tokens, 32 query heads on 8 KV heads of 128, 16 bits: the products
 // and their reads alone take 390 us, the softmax alone 250, staging adds 80; together 530-560 us (1.0 PFLOP/s), the matrix units
-// half busy at the 1.8 GHz that power allows then.  64 columns a wave would halve the reads, but their 512 registers leave one
-// wave a SIMD, which took twice as long.
+// half busy.  64 columns a wave would halve the reads, but their 512 registers leave one wave a SIMD, which took twice as long.
 #define PAGED_TILE 64
 
 // The tile of columns that a workgroup takes: sequence and first column, or b = n_seqs.  Sequences of more than `few`
