@@ -147,6 +147,19 @@ def test_arguments_that_are_refused(lib):
         assert calls(lib, batch=b, **kw)[2] == E
 
 
+@pytest.mark.parametrize("max_new,n_seqs", [(1, 4), (9, 1), (4, 4), (200, 1), (200, 4)])
+@pytest.mark.parametrize("D,bits", [(128, 16), (64, 4)])
+def test_work_space_that_is_refused(lib, max_new, n_seqs, D, bits):
+    """Batches that are cut into splits: without the work space, with one that is not aligned or a byte short nothing is launched."""
+    cfg = R.RkvPagedConfig(8, 2, 400, head_dim=D, bits=bits)
+    batch = a_batch(n_seqs=n_seqs, n_rows=max_new + 3, max_new=max_new, max_pages=100, max_len=6000)
+    need, c = C.c_size_t(), cfg.to_c()
+    assert lib.rkv_paged_scratch(C.byref(c), C.byref(batch), C.byref(need)) == B.RKV_OK and need.value > 1 << 16
+    for kw in (dict(scratch=None, scratch_bytes=need.value), dict(scratch=FAKE + 16, scratch_bytes=need.value), dict(scratch=FAKE + 128, scratch_bytes=1 << 40),
+               dict(scratch_bytes=need.value - 1), dict(scratch_bytes=0)):
+        assert calls(lib, cfg, batch, qs=8 * D, **kw)[2] == B.RKV_EINVAL
+
+
 def test_no_rows_is_nothing_to_do(lib):
     b = a_batch(n_rows=0, max_new=0, dev_page_table=None)
     assert calls(lib, batch=b, pool=None, k=None, v=None, q=None, out=None, scratch=None, scratch_bytes=0) == [B.RKV_OK] * 3

@@ -366,6 +366,34 @@ def test_queries_that_are_not_finite_touch_only_their_row():
     assert torch.equal(out[same], out0[same]) and torch.isnan(out[~same]).all()
 
 
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("long", [False, True], ids=["whole", "splits"])
+@pytest.mark.parametrize("news", [[5, 1], [14, 2], [8, 40]], ids=str)
+@pytest.mark.parametrize("bits,dtype,D", [(16, "fp16", 128), (16, "bf16", 64), (8, "bf16", 128), (8, "fp16", 64), (4, "fp16", 128), (4, "bf16", 64)])
+def test_what_drafted_tokens_do_not_see(bits, dtype, D, news, long, bad):
+    """As above for few rows: up to 16 and 32 columns and beside a chunk, in one span and in splits.  The spoilt key and value lie between the
+    first and the last new row's positions."""
+    lens = [1401, 700] if long else [150, 90]
+    made = [Setup(lens, hq=4, hkv=2, D=D, bits=bits, dtype=dtype, seed=9) for _ in range(2)]
+    n, m = lens[0], news[0]
+    made[1].k[0][n - 3, 0, 5] = bad                            # rows m - 3 .. see it
+    made[1].v[0][n - 2, 1, 40] = bad                           # rows m - 2 ..
+    out0, lse0, q = run(made[0], lens, news)
+    s = made[1]
+    s.fill()
+    out, lse = s.cache.attention(q, s.batch(lens, news), want_lse=True)
+    assert torch.equal(out[:m - 3], out0[:m - 3]) and torch.equal(lse[:m - 3], lse0[:m - 3])
+    assert torch.equal(out[m:], out0[m:]) and torch.equal(lse[m:], lse0[m:])
+    assert torch.equal(out[m - 3, 2:], out0[m - 3, 2:]) and torch.equal(lse[:, 2:], lse0[:, 2:])
+    channel = slice(40, 41) if bits == 16 else slice(32, 64)
+    rest = torch.ones(D, dtype=torch.bool)
+    rest[channel] = False
+    assert not torch.isfinite(out[m - 2:m, 2:, channel]).any()
+    assert torch.equal(out[m - 2:m, 2:][..., rest], out0[m - 2:m, 2:][..., rest])
+    if bits < 16 or np.isnan(bad):
+        assert torch.isnan(out[m - 3:m, :2]).all() and torch.isnan(lse[m - 3:m, :2]).all()
+
+
 def test_pages_outside_the_pool():
     """Tokens of such pages are not written and read as NaN; rows that see them are NaN, the others are not touched."""
     lens, news = [100, 50], [60, 1]
@@ -402,6 +430,41 @@ def test_sequences_beyond_the_hosts_bounds(what):
     assert torch.isnan(k[:5]).all() and torch.isnan(v[:5]).all() and torch.isfinite(k[5:]).all()
     out, lse = s.cache.attention(q, b, want_lse=True)
     assert torch.isnan(out[:5]).all() and torch.isnan(lse[:5]).all() and torch.equal(out[5:], out0[5:]) and torch.equal(lse[5:], lse0[5:])
+
+
+@pytest.mark.parametrize("what", ["length", "negative", "rows"])
+@pytest.mark.parametrize("news,which", [([150, 1, 5], 0), ([150, 1, 5], 2), ([90, 40, 2], 1), ([100, 4, 7], 1), ([9, 1, 4], 0), ([1, 10, 4], 1), ([3, 2, 5], 2),
+                                        ([150], 0), ([6], 0)], ids=str)
+def test_sequences_beyond_the_hosts_bounds_in_every_kernel(news, which, what):
+    """Three columns a row, which tiles of 256 do not divide; spans that are cut into splits; the bad sequence in either kernel and alone.
+    Its rows are NaN, its neighbours' as they are without it, rows of nobody untouched."""
+    lens = [1400, 1333, 1290][:len(news)]
+    s = Setup(lens, hq=6, hkv=2, bits=8, page=32, seed=sum(news))
+    s.fill()
+    told, kw = list(lens), dict(max_len=1400, max_new=max(news))
+    if what == "rows":                                         # one row more than the host said; the others keep to it
+        kw["max_new"] = news[which] - 1
+        news = [m if b == which else min(m, kw["max_new"]) for b, m in enumerate(news)]
+    else:
+        told[which] = 1401 if what == "length" else -2
+    q = torch.cat([s.noise(m, 6) for m in news] + [s.noise(3, 6)]).to(DEV)
+    out = torch.full_like(q, 5.0)
+    lse = torch.full(q.shape[:2], 5.0, device=DEV)
+    s.cache.attention(q, s.batch(told, news, extra=3, **kw), out=out, lse=lse)
+    row = 0
+    for b, m in enumerate(news):
+        if b == which:
+            assert torch.isnan(out[row:row + m]).all() and torch.isnan(lse[row:row + m]).all()
+        else:
+            one = [m if c == b else 0 for c in range(len(news))]
+            check_attention(s, lens, one, out, lse, q, rows_from=row)
+        row += m
+    assert (out[row:] == 5).all() and (lse[row:] == 5).all()
+    if what != "rows":                                         # the same launch without the fault
+        good, gl = s.cache.attention(q, s.batch(lens, news, extra=3, **kw), want_lse=True)
+        keep = torch.ones(row, dtype=torch.bool)
+        keep[sum(news[:which]):sum(news[:which + 1])] = False
+        assert torch.equal(out[:row][keep], good[:row][keep]) and torch.equal(lse[:row][keep], gl[:row][keep])
 
 
 def test_row_starts_that_make_no_sense():
@@ -499,6 +562,49 @@ def test_captured_steps_follow_the_lengths(news):
         junk = torch.randn(1 << 20, device=DEV).sum().item()   # the allocator's memory in use by others between replays
         check_attention(s, have, news, out, None, q)
         assert torch.equal(out, s.cache.attention(q, b)) and np.isfinite(junk)
+
+
+@pytest.mark.parametrize("starts", [[[0, 3, 8], [0, 6, 8], [2, 2, 8], [1, 7, 7], [0, 1, 2]], [[0, 40, 44], [0, 4, 44], [3, 3, 30], [0, 44, 44], [20, 21, 22]]],
+                         ids=["few", "chunk"])
+def test_captured_steps_follow_rows_and_pages(starts):
+    """Between replays rows move from one sequence to the other and pages to other places of the pool."""
+    lens = [900, 640]
+    s = Setup(lens, hq=8, hkv=2, bits=8, page=16, seed=17)
+    s.fill()
+    n = max(x[2] for x in starts)
+    b = R.RkvPagedBatch(s.dtable, ints(starts[0]), ints(lens), n_rows=n, max_new=max(max(x[1] - x[0], x[2] - x[1]) for x in starts), max_len=900)
+    k, v = (torch.zeros(n, 2, 128, dtype=torch.float16, device=DEV) for _ in range(2))
+    q, out = torch.zeros(n, 8, 128, dtype=torch.float16, device=DEV), torch.zeros(n, 8, 128, dtype=torch.float16, device=DEV)
+
+    def step():
+        s.cache.append(k, v, b)
+        s.cache.attention(q, b, out=out)
+    b.lengths.zero_()                                          # (rows in front of the first token: nothing is written)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i, at in enumerate(starts):
+        have = [900 - 7 * i, 640 - 100 * i]
+        news = [at[1] - at[0], at[2] - at[1]]
+        b.row_start.copy_(ints(at))
+        b.lengths.copy_(ints(have))
+        pages = s.cache.mem.view(s.n_pages, -1)                # every page moves on by one place
+        pages.copy_(pages.roll(1, 0))
+        used = s.dtable >= 0
+        s.dtable[used] = (s.dtable[used] + 1) % s.n_pages
+        k[at[0]:at[2]] = s.rows(s.k, have, news)
+        v[at[0]:at[2]] = s.rows(s.v, have, news)
+        q.copy_(s.noise(n, 8))
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        junk = torch.randn(1 << 20, device=DEV).sum().item()
+        check_attention(s, have, news, out, None, q, rows_from=at[0])
+        assert torch.isnan(out[:at[0]]).all() and torch.isnan(out[at[2]:]).all()
+        again = s.cache.attention(q, b)
+        assert torch.equal(out[at[0]:at[2]], again[at[0]:at[2]]) and np.isfinite(junk)
 
 
 def test_two_graphs_and_streams_at_once():
