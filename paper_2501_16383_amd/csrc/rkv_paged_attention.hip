@@ -53,6 +53,13 @@ template <int DT> __device__ __forceinline__ bool paged_odd(uint32_t x) {
   return (x & ex) == ex;
 }
 
+// Queries for a scale of zero: what is not finite as NaN, everything else as 0 - a score that is a number then is 0, also where the
+// unscaled one would pass fp32
+template <int DT> __device__ __forceinline__ uint32_t paged_times_zero(uint32_t x) {
+  constexpr uint32_t nan = DT ? 0x7fc0 : 0x7e00;
+  return (paged_odd<DT>(x) ? nan : 0) | (paged_odd<DT>(x >> 16) ? nan << 16 : 0);
+}
+
 __device__ __forceinline__ float paged_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Weights are held times a power of two that the division by their sum takes out again: in fp16 the largest is
@@ -177,6 +184,9 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 2) void k_paged_few(PagedView v,
       const int ch = BITS == 16 ? 32 * j + 8 * g : g * (D / 4) + 8 * j;
       const u32x4 z = {0, 0, 0, 0};
       q[i][j] = on ? *(const u32x4*)(a.q + (s.first + row) * a.qs + (kvh * v.rep + c % v.rep) * D + ch) : z;
+      if (a.scale2 == 0)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[i][j][e] = paged_times_zero<DT>(q[i][j][e]);
     }
   }
 
@@ -570,7 +580,9 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
     const u32x4 z = {0, 0, 0, 0};
     q[j] = mine ? *(const u32x4*)(a.q + (s.first + cc / v.rep) * a.qs + (kvh * v.rep + cc % v.rep) * D + 16 * j + 8 * h) : z;
     if (a.scale2 < 0) q[j] ^= 0x80008000u;                  // (the scale below is its magnitude)
-    if (a.scale2 == 0) q[j] = z;
+    if (a.scale2 == 0)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) q[j][e] = paged_times_zero<DT>(q[j][e]);
   }
   const float scale2 = a.scale2 == 0 ? 1.f : fabsf(a.scale2);
   f16v o[CB];

@@ -366,6 +366,29 @@ def test_queries_that_are_not_finite_touch_only_their_row():
     assert torch.equal(out[same], out0[same]) and torch.isnan(out[~same]).all()
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_a_scale_of_zero(dtype):
+    """Every score that is a number counts as 0, one of a query that is not finite is NaN, whichever kernel a sequence goes to;
+    bf16 queries whose products with the keys would pass fp32 are numbers."""
+    lens, news = [300, 90], [60, 2]                            # 240 columns, and 8
+    far = dtype == "bf16"
+    s = Setup(lens, hq=4, hkv=1, bits=16, dtype=dtype, scale_k=2.0**60 if far else 1.0, seed=1)
+    s.fill()
+    q = torch.cat([s.noise(m, 4) for m in news])
+    if far:
+        q[[25, 60]] = 2.0**100
+    clean = q.clone()
+    for row in (20, 61):
+        q[row, 0, 7], q[row, 1, 0], q[row, 2, 63] = np.nan, np.inf, -np.inf
+    out, lse = s.cache.attention(q.to(DEV), s.batch(lens, news), scale=0.0, want_lse=True)
+    odd = torch.zeros(62, 4, dtype=torch.bool)
+    odd[20, :3] = odd[61, :3] = True
+    assert torch.isnan(out[odd]).all() and torch.isnan(lse[odd]).all()
+    want, wl = s.cache.attention(torch.zeros_like(clean).to(DEV), s.batch(lens, news), scale=1.0, want_lse=True)
+    check_attention(s, lens, news, want, wl, torch.zeros_like(clean))
+    assert torch.equal(out[~odd], want[~odd]) and torch.equal(lse[~odd], wl[~odd])
+
+
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
 @pytest.mark.parametrize("long", [False, True], ids=["whole", "splits"])
 @pytest.mark.parametrize("news", [[5, 1], [14, 2], [8, 40]], ids=str)
