@@ -184,9 +184,6 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 2) void k_paged_few(PagedView v,
       const int ch = BITS == 16 ? 32 * j + 8 * g : g * (D / 4) + 8 * j;
       const u32x4 z = {0, 0, 0, 0};
       q[i][j] = on ? *(const u32x4*)(a.q + (s.first + row) * a.qs + (kvh * v.rep + c % v.rep) * D + ch) : z;
-      if (a.scale2 == 0)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) q[i][j][e] = paged_times_zero<DT>(q[i][j][e]);
     }
   }
 
@@ -400,6 +397,13 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 2) void k_paged_few(PagedView v,
     load_values(first);
     load_keys(first);
   }
+  if (a.scale2 == 0)
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < NK; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[i][j][e] = paged_times_zero<DT>(q[i][j][e]);
   for (int t = first; t < to; t += 128) compute(t, t + 128 < to);
 
   // the four waves meet
@@ -579,10 +583,6 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
   for (int j = 0; j < NS; ++j) {
     const u32x4 z = {0, 0, 0, 0};
     q[j] = mine ? *(const u32x4*)(a.q + (s.first + cc / v.rep) * a.qs + (kvh * v.rep + cc % v.rep) * D + 16 * j + 8 * h) : z;
-    if (a.scale2 < 0) q[j] ^= 0x80008000u;                  // (the scale below is its magnitude)
-    if (a.scale2 == 0)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) q[j][e] = paged_times_zero<DT>(q[j][e]);
   }
   const float scale2 = a.scale2 == 0 ? 1.f : fabsf(a.scale2);
   f16v o[CB];
@@ -820,6 +820,12 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
         k2 = k2 == 2 ? 0 : k2 + 1;                          // (the buffer of tile i + 3 is tile i's)
       }
       return;
+    }
+    if (a.scale2 <= 0) {                                    // (scale2 is its magnitude, or 1)
+#pragma unroll
+      for (int j = 0; j < NS; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[j][e] = a.scale2 < 0 ? q[j][e] ^ 0x80008000u : paged_times_zero<DT>(q[j][e]);
     }
     scores(lk[0], s0);
     auto walk = [&](auto masked, int end) PAGED_INLINE {
