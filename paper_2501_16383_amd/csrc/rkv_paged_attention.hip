@@ -7,7 +7,6 @@
 // the weights a lane gets from the first product are, in their order, an operand of the second.
 // (Which token is which index of the sum is free as long as both operands agree.)  Weights are powers of two of
 // scores in fp32; the sum of weights is taken in fp32 from unrounded weights.
-#include <cfloat>
 #include <type_traits>
 
 #include "rkv_mfma_ops.h"
@@ -66,8 +65,22 @@ __device__ __forceinline__ float paged_exp2(float x) { return __builtin_amdgcn_e
 // 2^14, so that one of 2^-28 of it still is a normal number (as a subnormal of 2^-25 it would be off by up to its own size).
 template <int DT> __device__ constexpr float paged_bias() { return DT ? 0.f : 14.f; }
 
-// ... in k_paged_chunk, where weights may pass the largest by 2^8
+// The exponent that weights are taken against where the largest score's is `top`.  From 2^24 on fp32's numbers lie 2 and more
+// apart: where the difference comes out as 16, 2^16 would be no fp16 number, and the largest weight is 1.
+template <int DT> __device__ __forceinline__ float paged_ref(float top) {
+  const float r = top - paged_bias<DT>();
+  return top - r > 15.f ? top : r;
+}
+
+// The exponent of the same power in k_paged_chunk, where weights may pass the largest by 2^8
 template <int DT> __device__ constexpr float paged_chunk_bias() { return DT ? 0.f : 6.f; }
+
+// score times scale, rounded, less `ref`: not one operation, which would leave the product's rounding in the difference
+__device__ __forceinline__ float paged_less(float score, float scale, float ref) {
+#pragma clang fp contract(off)
+  const float x = score * scale;
+  return x - ref;
+}
 
 // the value of the lane 32 further
 __device__ __forceinline__ float paged_other(float x, float& mine) {
@@ -91,7 +104,7 @@ __device__ __forceinline__ float paged_sum4(float x) {
 }
 
 // Splits of the sequences' tokens: partial results of a work unit (a sequence's columns or a tile of them, and a KV
-// head), as acc [unit][column][split][D] and then (maximum, sum) [unit][column][split]
+// head), as acc [unit][column][split][D] and then (exponent that weights are taken against, their sum) [unit][column][split]
 struct PagedSplit {
   int chunk, splits;                  // tokens of a split, most splits of a sequence
   float* acc;
@@ -111,8 +124,9 @@ struct PagedAsk {
   PagedSplit sp;
 };
 
-template <int DT> __device__ __forceinline__ float paged_lse(float m, float sum) {
-  return sum == 0 ? -INFINITY : (m + __log2f(sum) - paged_bias<DT>()) * 0.69314718055994531f;
+// Log-sum-exp of a sum of weights against 2^ref, times 2^bias
+__device__ __forceinline__ float paged_lse(float ref, float sum, float bias) {
+  return sum == 0 ? -INFINITY : (ref + (__log2f(sum) - bias)) * 0.69314718055994531f;
 }
 
 // Tokens that the row at position p sees: lo .. hi - 1 (none in front of the first token)
@@ -188,7 +202,7 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 2) void k_paged_few(PagedView v,
   }
 
   f4 o[NB][CB];
-  float m[NB], l[NB];
+  float m[NB], l[NB];                                       // what weights are taken against (paged_ref), their sum
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
     m[i] = -INFINITY;
@@ -333,14 +347,14 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 2) void k_paged_few(PagedView v,
       }
       float top = fmaxf(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])), fmaxf(fmaxf(w[4], w[5]), fmaxf(w[6], w[7])));
       top = paged_max4(top);
-      if (__any(top > m[c])) {
-        const float m2 = fmaxf(m[c], top), f = m2 == m[c] ? 1.f : paged_exp2(m[c] - m2);
+      if (__any(top - paged_bias<DT>() > m[c])) {
+        const float m2 = fmaxf(m[c], paged_ref<DT>(top)), f = m2 == m[c] ? 1.f : paged_exp2(m[c] - m2);
         m[c] = m2;
         l[c] *= f;
 #pragma unroll
         for (int k = 0; k < CB; ++k) o[c][k] *= f;
       }
-      const float ref = (m[c] == -INFINITY ? 0.f : m[c]) - paged_bias<DT>();
+      const float ref = m[c] == -INFINITY ? 0.f : m[c];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         w[e] = paged_exp2(w[e] - ref);
@@ -435,7 +449,7 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 2) void k_paged_few(PagedView v,
       const int64_t at = (int64_t)(s.first + cc / v.rep) * v.Hq + kvh * v.rep + cc % v.rep;
       if (a.sp.splits == 1) {
         a.out[at * D + ch] = (unsigned short)paged_pair<DT>(sum == 0 ? 0.f : acc / sum, 0.f);
-        if (a.lse && ch == 0) a.lse[at] = paged_lse<DT>(mm, sum);
+        if (a.lse && ch == 0) a.lse[at] = paged_lse(mm, sum, 0);
       } else {
         const int64_t u = (((int64_t)b * v.Hkv + kvh) * (16 * NB) + cc) * a.sp.splits + split;
         a.sp.acc[u * D + ch] = acc;
@@ -479,7 +493,7 @@ template <int D, int DT> __device__ __forceinline__ void paged_join(const PagedA
   }
 #pragma unroll
   for (int j = 0; j < C; ++j) a.out[at * D + lane + 64 * j] = (unsigned short)paged_pair<DT>(sum == 0 ? 0.f : acc[j] / sum, 0.f);
-  if (a.lse && lane == 0) a.lse[at] = paged_lse<DT>(m, sum);
+  if (a.lse && lane == 0) a.lse[at] = paged_lse(m, sum, 0);
 }
 
 template <int D, int DT, int NB>
@@ -586,7 +600,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
   }
   const float scale2 = a.scale2 == 0 ? 1.f : fabsf(a.scale2);
   f16v o[CB];
-  float m = -INFINITY, l = 0;
+  float m = -INFINITY, l = 0, worst = 0;                    // worst: largest magnitude that m had
 #pragma unroll
   for (int k = 0; k < CB; ++k) o[k] = f16v{};
 
@@ -754,10 +768,11 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
     float own;
     const float other = paged_other(top, own);
     top = fmaxf(own, other) * scale2;
-    const bool up = top > fmaxf(m + SLACK, -FLT_MAX);       // (after none, any score is a new maximum)
+    const bool up = top - m > SLACK;                        // (after none, any score is a new maximum)
     const float m2 = up ? top : m, f = up ? paged_exp2(m - m2) : 1.f;
     const float ref = paged_chunk_bias<DT>() - (m2 == -INFINITY ? 0.f : m2);
     m = m2;
+    worst = fmaxf(worst, fabsf(ref));
     __builtin_amdgcn_s_setprio(1);                          // (the other wave of the SIMD has its arithmetic meanwhile)
     scores(kb, next);
     float sum = 0;
@@ -861,6 +876,79 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
     else values(std::false_type{}, lv[vb] + 32 * PV, p1, t + 32);
   }
 
+  // A weight above is the power of one multiplication and addition, whose error against the rounded maximum grows with the maximum: from
+  // 2^25 on fp16 weights would pass their type.  Columns that were beyond 2^20, which are rare, are taken anew: token after token from memory,
+  // differences of scores that are rounded alike, weights in fp32.  (Asking for such a maximum in the loop takes
+  // 1.5-2.4 % of every call; this way a prompt of 8192 tokens takes 24 ms if all its rows are such.)
+  const bool far = worst > 0x1p20f && m != INFINITY;
+  if (m == INFINITY) l = NAN;                               // (a score of infinity: infinity less infinity)
+  if (__builtin_expect(__any(far), 0)) {
+    if (far) {
+      m = -INFINITY;
+      l = 0;
+#pragma unroll
+      for (int k = 0; k < CB; ++k) o[k] = f16v{};
+    }
+#pragma unroll 1
+    for (int t = from; t < to; ++t) {
+      const int pg = table[t >> v.page_shift], slot = t & mask;
+      const bool ok = (unsigned)pg < (unsigned)v.n_pages;
+      const unsigned char* blk = pool + (ok ? pg : 0) * page_bytes;
+      const unsigned char *kd = blk + slot * rb, *sd = blk + ((2 * rb) << v.page_shift) + slot * sb;
+      const unsigned char *vd = kd + (rb << v.page_shift), *vsd = sd + (sb << v.page_shift);
+      float x = 0;
+#pragma unroll
+      for (int j = 0; j < NS; ++j) {                        // this lane's half of the channels
+        const unsigned char* at = kd + (16 * j + 8 * h) * BITS / 8;
+        u32x4 kk;
+        if constexpr (BITS == 16) kk = *(const u32x4*)at;
+        else {
+          u32x2 c = {0, 0};
+          if constexpr (BITS == 8) c = *(const u32x2*)at;
+          else c[0] = *(const uint32_t*)at;
+          kk = paged_decode8<DT, BITS>(c, paged_scale(sd[j >> 1]));
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x = __builtin_fmaf(paged_lo<DT>(kk[e]), paged_lo<DT>(q[j][e]), x);
+          x = __builtin_fmaf(paged_hi<DT>(kk[e]), paged_hi<DT>(q[j][e]), x);
+        }
+      }
+      float half;
+      const float rest = paged_other(x, half);
+      x = ok ? (half + rest) * scale2 : NAN;
+      if (far && t >= lo && t < hi) {
+        const float m2 = fmaxf(m, x), base = m2 == -INFINITY ? 0.f : m2, f = m2 == m ? 1.f : paged_exp2(m - m2);
+        const float w = paged_exp2(paged_less(x, 1.f, base));
+        m = m2;
+        l = l * f + w;
+#pragma unroll
+        for (int k = 0; k < CB; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const unsigned char* at = vd + (32 * k + 8 * i + 4 * h) * BITS / 8;
+            u32x2 vv;
+            if constexpr (BITS == 16) vv = *(const u32x2*)at;
+            else {
+              const uint32_t c = BITS == 8 ? *(const uint32_t*)at : *(const unsigned short*)at;
+              const float sc = paged_scale(vsd[k]);
+              vv = u32x2{paged_decode2<DT, BITS, 0>(c, sc), paged_decode2<DT, BITS, 1>(c, sc)};
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              o[k][4 * i + 2 * e] = __builtin_fmaf(w, paged_lo<DT>(vv[e]), o[k][4 * i + 2 * e] * f);
+              o[k][4 * i + 2 * e + 1] = __builtin_fmaf(w, paged_hi<DT>(vv[e]), o[k][4 * i + 2 * e + 1] * f);
+            }
+          }
+      }
+    }
+    if (far) {
+      constexpr float unit = DT ? 1.f : 64.f;               // 2^bias, as the other columns
+      l = h == 0 ? l * unit : 0.f;                          // (the two lanes of a column are added below)
+#pragma unroll
+      for (int k = 0; k < CB; ++k) o[k] *= unit;
+    }
+  }
   float own;
   const float other = paged_other(l, own), sum = own + other;
   if (!mine) return;
@@ -873,7 +961,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
         const u32x2 w = {paged_pair<DT>(o[k][4 * e] * inv, o[k][4 * e + 1] * inv), paged_pair<DT>(o[k][4 * e + 2] * inv, o[k][4 * e + 3] * inv)};
         *(u32x2*)(a.out + at * D + 32 * k + 8 * e + 4 * h) = w;
       }
-    if (a.lse && h == 0) a.lse[at] = sum == 0 ? -INFINITY : (m + __log2f(sum) - paged_chunk_bias<DT>()) * 0.69314718055994531f;
+    if (a.lse && h == 0) a.lse[at] = paged_lse(m, sum, paged_chunk_bias<DT>());
   } else {
     const int64_t u = (((int64_t)unit * v.Hkv + kvh) * COLS + (cc - c0)) * a.sp.splits + split;
 #pragma unroll
@@ -881,8 +969,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_paged_chunk(PagedView v, PagedAs
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         *(f4*)(a.sp.acc + u * D + 32 * k + 8 * e + 4 * h) = f4{o[k][4 * e], o[k][4 * e + 1], o[k][4 * e + 2], o[k][4 * e + 3]};
-    // (as k_paged_few's: the merge knows one bias)
-    if (h == 0) a.sp.ml[u] = make_float2(m + (paged_bias<DT>() - paged_chunk_bias<DT>()), sum);
+    if (h == 0) a.sp.ml[u] = make_float2(m, sum);
   }
 }
 
@@ -937,7 +1024,7 @@ __global__ __launch_bounds__(256) void k_paged_chunk_merge(PagedView v, PagedAsk
     const int64_t at = (int64_t)(s.first + (c0 + c) / v.rep) * v.Hq + kvh * v.rep + (c0 + c) % v.rep;
     const float inv = sum == 0 ? 0.f : 1.f / sum;
     *(u32x2*)(a.out + at * D + ch) = u32x2{paged_pair<DT>(acc[0] * inv, acc[1] * inv), paged_pair<DT>(acc[2] * inv, acc[3] * inv)};
-    if (a.lse && ch == 0) a.lse[at] = paged_lse<DT>(mm, sum);
+    if (a.lse && ch == 0) a.lse[at] = paged_lse(mm, sum, paged_chunk_bias<DT>());
   }
 }
 

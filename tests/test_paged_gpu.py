@@ -389,6 +389,69 @@ def test_a_scale_of_zero(dtype):
     assert torch.equal(out[~odd], want[~odd]) and torch.equal(lse[~odd], wl[~odd])
 
 
+@pytest.mark.parametrize("news", [[3, 1], [10, 1], [20, 1], [70, 2]], ids=str)
+@pytest.mark.parametrize("bits,dtype,D,e,scale", [(16, t, 64, e, np.log(2)) for t in ("fp16", "bf16") for e in (20, 23, 24, 25, 26, 27, 28)]
+                         + [(b, t, 64 if b == 8 else 128, e, np.log(2)) for b in (8, 4) for t in ("fp16", "bf16") for e in (24, 27)]
+                         + [(16, "fp16", 128, 29, 1.0), (16, "fp16", 64, 29, -1.0), (8, "bf16", 128, 33, 1.0), (16, "bf16", 128, 40, 1.0)])
+def test_scores_so_large_that_fp32_holds_few_of_them(bits, dtype, D, e, scale, news):
+    """Scores 2^e + j 2^(e - 23): neighbours in fp32, from two channels whose products and sum are exact.  With a scale of log(2), a
+    power of two's exponent is the score itself, so that the weights are exact powers; with 1, whose scaled scores are rounded, j goes in steps of 4:
+    two scores are the same or further apart than any weight reaches.  So no error of a score counts in the bound, and what a
+    weight's rounding to fp16's subnormal numbers costs is at most 2^-25 of the largest weight, which is 1 or more (header).
+    Rows of small queries stand among them and have the bits that they have alone."""
+    lens = [700, 130]
+    s = Setup(lens, hq=2, hkv=1, D=D, bits=bits, dtype=dtype, seed=e)
+    for k in s.k:
+        k.zero_()
+        k[:, 0, 0] = 2.0 ** (e - e // 2)
+        k[:, 0, 40] = torch.randint(0, 8, k.shape[:1], generator=s.g).to(k.dtype) * (1 if abs(scale) < 1 else 4)
+    s.fill()
+    q = torch.zeros(sum(news), 2, D, dtype=TYPES[dtype])
+    q[..., 0], q[..., 40] = 2.0 ** (e // 2) * np.sign(scale), 2.0 ** (e - 23) * np.sign(scale)
+    near = q * 2.0**-30
+    out, lse = (x.cpu().double().numpy() for x in s.cache.attention(q.to(DEV), s.batch(lens, news), scale=scale, want_lse=True))
+    u, least = (2.0**-11, 2.0**-25) if dtype == "fp16" else (2.0**-8, 0)
+    row = 0
+    for b, (n, m) in enumerate(zip(lens, news)):
+        ref, rl, spread, _, mass = O.attention(q[row:row + m].double().numpy(), s.held(s.k, b, n), s.held(s.v, b, n), n - m, scale=scale)
+        assert np.isfinite(out[row:row + m]).all() and np.isfinite(lse[row:row + m]).all()
+        tol = spread * (u + (n + 16) * 2.0**-24) * 1.001 + u * np.abs(ref) + 2.0**-25 + mass * least
+        assert (np.abs(out[row:row + m] - ref) <= tol).all(), (b, (np.abs(out[row:row + m] - ref) / tol).max())
+        assert (np.abs(lse[row:row + m] - rl) <= np.abs(rl) * 2.0**-22).all()
+        row += m
+    few = torch.arange(sum(news)) % 3 != 1
+    mixed = torch.where(few[:, None, None], q, near).to(DEV)
+    a, b = (s.cache.attention(x, s.batch(lens, news), scale=scale, want_lse=True) for x in (mixed, near.to(DEV)))
+    assert torch.equal(a[0][~few], b[0][~few]) and torch.equal(a[1][~few], b[1][~few])
+    assert np.array_equal(a[0][few].cpu().double().numpy(), out[few.numpy()])
+
+
+def test_large_scores_and_what_is_no_number():
+    """Rows whose scores are large, over a page outside the pool, a NaN key and an infinite one: NaN from there on, and the rows in front
+    and the other KV head's as they are without."""
+    lens, news = [300, 40], [90, 1]
+    made = [Setup(lens, hq=4, hkv=2, bits=16, seed=2, scale_k=64.0) for _ in range(2)]
+    for s in made:
+        s.fill()
+    s = made[0]
+    q = (torch.cat([s.noise(m, 4) for m in news]) * 2048.0).to(DEV)
+    out0, lse0 = s.cache.attention(q, s.batch(lens, news), scale=16.0, want_lse=True)
+    assert torch.isfinite(out0).all() and torch.isfinite(lse0).all() and (lse0.abs() > 2**20).any()
+    s.dtable[0, 16] = -1                                       # tokens 256 ..: rows 46 ..
+    out, lse = s.cache.attention(q, s.batch(lens, news), scale=16.0, want_lse=True)
+    assert torch.equal(out[:46], out0[:46]) and torch.equal(lse[:46], lse0[:46]) and torch.isnan(out[46:90]).all() and torch.isnan(lse[46:90]).all()
+    assert torch.equal(out[90], out0[90])
+    for bad in (np.nan, np.inf):
+        s = made[1]
+        s.k[0][256, 0, 5] = bad
+        s.fill()
+        out, lse = s.cache.attention(q.abs(), s.batch(lens, news), scale=16.0, want_lse=True)
+        want, wl = made[0].cache.attention(q.abs(), R.RkvPagedBatch(made[0].table.to(DEV), ints([0, 90, 91]), ints(lens), 91, max_new=90), scale=16.0,
+                                           want_lse=True)
+        assert torch.equal(out[:46], want[:46]) and torch.equal(lse[:46], wl[:46]) and torch.equal(out[:, 2:], want[:, 2:])
+        assert torch.isnan(out[46:90, :2]).all() and torch.isnan(lse[46:90, :2]).all()
+
+
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
 @pytest.mark.parametrize("long", [False, True], ids=["whole", "splits"])
 @pytest.mark.parametrize("news", [[5, 1], [14, 2], [8, 40]], ids=str)
