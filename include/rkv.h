@@ -354,7 +354,10 @@ typedef struct rkv_paged_config {
  *   - a token whose page number is outside 0..n_pages - 1 is not written and reads as NaN, as does the
  *     attention of every row that sees it;
  *   - a row in front of its sequence's first token (more rows than tokens) is not written, reads as zero and
- *     sees nothing. */
+ *     sees nothing.
+ * Refused (RKV_EINVAL) as more than a launch holds: n_rows * n_q_heads above 2^30; n_rows * n_kv_heads * head_dim
+ * above 2^35 - 2048 in append and read; and in attention, with max_new * rep above 32 (rep = n_q_heads / n_kv_heads),
+ * n_kv_heads * (n_rows * rep / 256 + the smaller of n_seqs and n_rows * rep / 16) from 2^23 on. */
 typedef struct rkv_paged_batch {
   const int32_t* dev_page_table;  /* [n_seqs][max_pages]; entries behind a sequence's last token are not used */
   const int32_t* dev_row_start;   /* [n_seqs + 1], ascending from >= 0 to <= n_rows                */

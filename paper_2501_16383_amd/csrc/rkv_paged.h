@@ -4,6 +4,7 @@
 #include "rkv_internal.h"
 
 #define RKV_PAGED_BLOCK 32            // channels that share a scale
+#define RKV_PAGED_THREADS (1ll << 32)  // threads that a launch has not, in each direction of its grid
 
 struct PagedView {
   unsigned char* pool;
@@ -111,6 +112,7 @@ __device__ __forceinline__ int paged_page(const PagedView& v, int b, int t) {
 
 int rkv_launch_paged_append(const PagedView& v, int D, int bits, int dtype, const void* k, int64_t ks, const void* v_, int64_t vs, hipStream_t s);
 int rkv_launch_paged_read(const PagedView& v, int D, int bits, int dtype, void* k, int64_t ks, void* v_, int64_t vs, hipStream_t s);
+bool rkv_paged_attention_fits(const PagedView& v);       // do its launches stay under RKV_PAGED_THREADS?
 size_t rkv_paged_attention_scratch(const PagedView& v, int D, int bits);
 int rkv_launch_paged_attention(const PagedView& v, int D, int bits, int dtype, const void* q, int64_t qs, int causal, int window, float scale,
                                void* out, float* lse, void* scratch, hipStream_t s);

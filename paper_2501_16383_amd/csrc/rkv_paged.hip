@@ -239,7 +239,7 @@ static int check_batch(const rkv_paged_config* c, const rkv_paged_batch* b, void
   if (b->n_seqs < 1 || b->n_seqs > 65535 || b->max_pages < 1) return RKV_EINVAL;
   if (b->max_new < 1 || b->max_new > b->n_rows) return RKV_EINVAL;
   if (b->max_len < 1 || b->max_len > 1 << 30 || b->max_len > (int64_t)b->max_pages * c->page_tokens) return RKV_EINVAL;
-  if ((int64_t)b->n_rows * c->n_q_heads > (int64_t)1 << 30) return RKV_EINVAL;   // (the launches' grids)
+  if ((int64_t)b->n_rows * c->n_q_heads > (int64_t)1 << 30) return RKV_EINVAL;   // (rows and columns are counted in 32 bits)
   if ((uintptr_t)pool & 15) return RKV_EINVAL;
   v->pool = (unsigned char*)pool;
   v->table = b->dev_page_table;
@@ -277,6 +277,7 @@ RKV_EXPORT int rkv_paged_append(const rkv_paged_config* cfg, void* dev_pool, con
   const int rc = check_batch(cfg, batch, dev_pool, &v);
   if (rc != RKV_OK || v.n_rows == 0) return rc;
   if (!dev_pool || !rows_ok(cfg, dev_k, k_stride, cfg->n_kv_heads) || !rows_ok(cfg, dev_v, v_stride, cfg->n_kv_heads)) return RKV_EINVAL;
+  if (move_blocks(v, cfg->head_dim) * 256 >= RKV_PAGED_THREADS) return RKV_EINVAL;
 #define ARGS v, cfg->dtype, dev_k, k_stride, dev_v, v_stride, (hipStream_t)stream
   PAGED_DISPATCH(launch_append);
 #undef ARGS
@@ -290,6 +291,7 @@ RKV_EXPORT int rkv_paged_read(const rkv_paged_config* cfg, const void* dev_pool,
   const int rc = check_batch(cfg, batch, (void*)dev_pool, &v);
   if (rc != RKV_OK || v.n_rows == 0) return rc;
   if (!dev_pool || !rows_ok(cfg, dev_k, k_stride, cfg->n_kv_heads) || !rows_ok(cfg, dev_v, v_stride, cfg->n_kv_heads)) return RKV_EINVAL;
+  if (move_blocks(v, cfg->head_dim) * 256 >= RKV_PAGED_THREADS) return RKV_EINVAL;
 #define ARGS v, cfg->dtype, dev_k, k_stride, dev_v, v_stride, (hipStream_t)stream
   PAGED_DISPATCH(launch_read);
 #undef ARGS
@@ -301,6 +303,7 @@ RKV_EXPORT int rkv_paged_scratch(const rkv_paged_config* cfg, const rkv_paged_ba
   PagedView v{};
   const int rc = check_batch(cfg, batch, nullptr, &v);
   if (rc != RKV_OK) return rc;
+  if (v.n_rows && !rkv_paged_attention_fits(v)) return RKV_EINVAL;
   if (scratch_bytes) *scratch_bytes = v.n_rows ? rkv_paged_attention_scratch(v, cfg->head_dim, cfg->bits) : 0;
   return RKV_OK;
 }
@@ -314,6 +317,7 @@ RKV_EXPORT int rkv_paged_attention(const rkv_paged_config* cfg, const void* dev_
   if ((causal != 0 && causal != 1) || window < 0 || !__builtin_isfinite(scale * 1.4426950408889634f)) return RKV_EINVAL;
   if (v.n_rows == 0) return RKV_OK;
   if (!dev_pool || !rows_ok(cfg, dev_q, q_stride, cfg->n_q_heads) || !dev_out || ((uintptr_t)dev_out & 15) || ((uintptr_t)dev_lse & 3)) return RKV_EINVAL;
+  if (!rkv_paged_attention_fits(v)) return RKV_EINVAL;
   const size_t need = rkv_paged_attention_scratch(v, cfg->head_dim, cfg->bits);
   if (need && (!dev_scratch || ((uintptr_t)dev_scratch & 255) || scratch_bytes < need)) return RKV_EINVAL;
   return rkv_launch_paged_attention(v, cfg->head_dim, cfg->bits, cfg->dtype, dev_q, q_stride, causal, window, scale, dev_out, dev_lse,

@@ -1074,6 +1074,7 @@ static int64_t chunk_units(const PagedView& v) {
   const int64_t cols = (int64_t)v.n_rows * v.rep, most = cols / RKV_PAGED_FEW_MIXED, seqs = v.n_seqs < most ? v.n_seqs : most;
   return (cols / RKV_PAGED_COLS + seqs) * v.Hkv;
 }
+bool rkv_paged_attention_fits(const PagedView& v) { return !has_chunk(v) || chunk_units(v) * 512 < RKV_PAGED_THREADS; }   // (k_paged_few's is Hkv x 256 x n_seqs)
 #define CHUNK_WANT RKV_PAGED_CUS
 #define CHUNK_STEP 512
 // work space: k_paged_few's partial results, then k_paged_chunk's

@@ -160,6 +160,21 @@ def test_work_space_that_is_refused(lib, max_new, n_seqs, D, bits):
         assert calls(lib, cfg, batch, qs=8 * D, **kw)[2] == B.RKV_EINVAL
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_batches_that_no_launch_holds(lib, D):
+    """2^32 threads and more: one for eight channels of a row in append and read, 512 for a tile of columns in attention."""
+    cfg, E = R.RkvPagedConfig(256, 256, 100, head_dim=D), 256 * D
+    rows = 2**35 // E                                          # rows * heads * D = 2^35
+    batch = a_batch(n_rows=rows, max_new=1)
+    assert calls(lib, cfg, batch, ks=E, vs=E, qs=8)[:2] == [B.RKV_EINVAL] * 2
+    batch = a_batch(n_rows=2**22, n_seqs=65535, max_new=100)   # (2^22 * 256 / 256 + 65535 * 256) workgroups of 512
+    assert calls(lib, cfg, batch, ks=8, vs=8, qs=E)[2] == B.RKV_EINVAL
+    n, c = C.c_size_t(77), cfg.to_c()
+    assert lib.rkv_paged_scratch(C.byref(c), C.byref(batch), C.byref(n)) == B.RKV_EINVAL and n.value == 77
+    batch.max_new = 32                                         # few rows: a workgroup for a sequence and head
+    assert lib.rkv_paged_scratch(C.byref(c), C.byref(batch), C.byref(n)) == B.RKV_OK
+
+
 def test_no_rows_is_nothing_to_do(lib):
     b = a_batch(n_rows=0, max_new=0, dev_page_table=None)
     assert calls(lib, batch=b, pool=None, k=None, v=None, q=None, out=None, scratch=None, scratch_bytes=0) == [B.RKV_OK] * 3
