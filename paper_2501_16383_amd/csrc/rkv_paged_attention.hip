@@ -41,8 +41,8 @@ __device__ __forceinline__ u32x2 paged_transposed(const unsigned short* p) {
 // builtin: after that one the compiler has every read of LDS wait for the copy, also those of other buffers.  It does
 // not know of this one: whoever reads waits for vmcnt(0) first (paged_copies_done) and meets the other waves at a barrier.
 __device__ __forceinline__ void paged_copy(const void* base, uint32_t offset, unsigned short* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               : : "s"((uint32_t)(uintptr_t)(LDS_AS unsigned short*)to), "v"(offset), "s"(base) : "memory");   // (m0 is nobody else's: the compiler sets it where it needs it)
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               : : "{m0}"((uint32_t)(uintptr_t)(LDS_AS unsigned short*)to), "v"(offset), "s"(base) : "memory");   // (m0: written by the compiler, which knows of it)
 }
 __device__ __forceinline__ void paged_copies_done() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
 
