@@ -110,8 +110,6 @@ __device__ __forceinline__ int paged_page(const PagedView& v, int b, int t) {
   return (unsigned)p < (unsigned)v.n_pages ? p : -1;
 }
 
-int rkv_launch_paged_append(const PagedView& v, int D, int bits, int dtype, const void* k, int64_t ks, const void* v_, int64_t vs, hipStream_t s);
-int rkv_launch_paged_read(const PagedView& v, int D, int bits, int dtype, void* k, int64_t ks, void* v_, int64_t vs, hipStream_t s);
 bool rkv_paged_attention_fits(const PagedView& v);       // do its launches stay under RKV_PAGED_THREADS?
 size_t rkv_paged_attention_scratch(const PagedView& v, int D, int bits);
 int rkv_launch_paged_attention(const PagedView& v, int D, int bits, int dtype, const void* q, int64_t qs, int causal, int window, float scale,
