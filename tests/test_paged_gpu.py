@@ -393,13 +393,14 @@ def test_a_scale_of_zero(dtype):
 @pytest.mark.parametrize("bits,dtype,D,e,scale", [(16, t, 64, e, np.log(2)) for t in ("fp16", "bf16") for e in (20, 23, 24, 25, 26, 27, 28)]
                          + [(b, t, 64 if b == 8 else 128, e, np.log(2)) for b in (8, 4) for t in ("fp16", "bf16") for e in (24, 27)]
                          + [(16, "fp16", 128, 29, 1.0), (16, "fp16", 64, 29, -1.0), (8, "bf16", 128, 33, 1.0), (16, "bf16", 128, 40, 1.0)])
-def test_scores_so_large_that_fp32_holds_few_of_them(bits, dtype, D, e, scale, news):
-    """Scores 2^e + j 2^(e - 23): neighbours in fp32, from two channels whose products and sum are exact.  With a scale of log(2), a
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_so_large_that_fp32_holds_few_of_them(bits, dtype, D, e, scale, news, sign):
+    """Scores 2^e + j 2^(e - 23), or less than 0 by as much: neighbours in fp32, from two channels whose products and sum are exact.  With a scale of log(2), a
     power of two's exponent is the score itself, so that the weights are exact powers; with 1, whose scaled scores are rounded, j goes in steps of 4:
     two scores are the same or further apart than any weight reaches.  So no error of a score counts in the bound, and what a
     weight's rounding to fp16's subnormal numbers costs is at most 2^-25 of the largest weight, which is 1 or more (header).
     Rows of small queries stand among them and have the bits that they have alone."""
-    lens = [700, 130]
+    lens, kw = [700, 130], dict(scale=scale, window=90 if e % 2 else 0)
     s = Setup(lens, hq=2, hkv=1, D=D, bits=bits, dtype=dtype, seed=e)
     for k in s.k:
         k.zero_()
@@ -407,13 +408,13 @@ def test_scores_so_large_that_fp32_holds_few_of_them(bits, dtype, D, e, scale, n
         k[:, 0, 40] = torch.randint(0, 8, k.shape[:1], generator=s.g).to(k.dtype) * (1 if abs(scale) < 1 else 4)
     s.fill()
     q = torch.zeros(sum(news), 2, D, dtype=TYPES[dtype])
-    q[..., 0], q[..., 40] = 2.0 ** (e // 2) * np.sign(scale), 2.0 ** (e - 23) * np.sign(scale)
+    q[..., 0], q[..., 40] = 2.0 ** (e // 2) * np.sign(scale) * sign, 2.0 ** (e - 23) * np.sign(scale) * sign
     near = q * 2.0**-30
-    out, lse = (x.cpu().double().numpy() for x in s.cache.attention(q.to(DEV), s.batch(lens, news), scale=scale, want_lse=True))
+    out, lse = (x.cpu().double().numpy() for x in s.cache.attention(q.to(DEV), s.batch(lens, news), want_lse=True, **kw))
     u, least = (2.0**-11, 2.0**-25) if dtype == "fp16" else (2.0**-8, 0)
     row = 0
     for b, (n, m) in enumerate(zip(lens, news)):
-        ref, rl, spread, _, mass = O.attention(q[row:row + m].double().numpy(), s.held(s.k, b, n), s.held(s.v, b, n), n - m, scale=scale)
+        ref, rl, spread, _, mass = O.attention(q[row:row + m].double().numpy(), s.held(s.k, b, n), s.held(s.v, b, n), n - m, **kw)
         assert np.isfinite(out[row:row + m]).all() and np.isfinite(lse[row:row + m]).all()
         tol = spread * (u + (n + 16) * 2.0**-24) * 1.001 + u * np.abs(ref) + 2.0**-25 + mass * least
         assert (np.abs(out[row:row + m] - ref) <= tol).all(), (b, (np.abs(out[row:row + m] - ref) / tol).max())
@@ -421,7 +422,7 @@ def test_scores_so_large_that_fp32_holds_few_of_them(bits, dtype, D, e, scale, n
         row += m
     few = torch.arange(sum(news)) % 3 != 1
     mixed = torch.where(few[:, None, None], q, near).to(DEV)
-    a, b = (s.cache.attention(x, s.batch(lens, news), scale=scale, want_lse=True) for x in (mixed, near.to(DEV)))
+    a, b = (s.cache.attention(x, s.batch(lens, news), want_lse=True, **kw) for x in (mixed, near.to(DEV)))
     assert torch.equal(a[0][~few], b[0][~few]) and torch.equal(a[1][~few], b[1][~few])
     assert np.array_equal(a[0][few].cpu().double().numpy(), out[few.numpy()])
 
@@ -478,6 +479,28 @@ def test_what_drafted_tokens_do_not_see(bits, dtype, D, news, long, bad):
     assert torch.equal(out[m - 2:m, 2:][..., rest], out0[m - 2:m, 2:][..., rest])
     if bits < 16 or np.isnan(bad):
         assert torch.isnan(out[m - 3:m, :2]).all() and torch.isnan(lse[m - 3:m, :2]).all()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("bits,dtype", [(16, "fp16"), (8, "bf16"), (4, "fp16")])
+@pytest.mark.parametrize("news", [[8, 1], [15, 2], [70, 5]], ids=str)
+def test_what_a_window_has_left_has_no_influence(news, bits, dtype, causal):
+    """A NaN key and an infinite value: rows whose window starts behind them, and, causal, rows in front of them, have the bits that they
+    have without."""
+    lens, window = [330, 200], 3 if news[0] < 20 else 20
+    made = [Setup(lens, hq=4, hkv=2, bits=bits, dtype=dtype, seed=4) for _ in range(2)]
+    n, m = lens[0], news[0]
+    at = n - m + 2
+    made[1].k[0][at, 0, 5], made[1].v[0][at, 1, 40] = np.nan, np.inf
+    out0, lse0, q = run(made[0], lens, news, causal=causal, window=window)
+    s = made[1]
+    s.fill()
+    out, lse = s.cache.attention(q, s.batch(lens, news), causal=causal, window=window, want_lse=True)
+    first, behind = 2 if causal else 0, 2 + window             # rows first .. behind - 1 see token `at`
+    clean = torch.ones(sum(news), dtype=torch.bool)
+    clean[first:behind] = False
+    assert clean[:m].any() and torch.equal(out[clean], out0[clean]) and torch.equal(lse[clean], lse0[clean])
+    assert torch.isnan(out[first:behind, :2]).all() and not torch.isfinite(out[first:behind, 2:, 40]).any()
 
 
 def test_pages_outside_the_pool():
