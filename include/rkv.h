@@ -377,7 +377,7 @@ int rkv_paged_sizes(const rkv_paged_config* cfg, size_t* pool_bytes);
  *   dev_k, dev_v   [n_rows][n_kv_heads][head_dim] of the cache's type, 16-byte aligned; rows lie k_stride /
  *              v_stride elements apart (a multiple of 8, at least n_kv_heads * head_dim: the two may be
  *              columns of one projection's output)
- * Two rows that name the same slot leave either's bytes there. */
+ * Where two rows name the same slot each of its bytes is one row's or the other's. */
 int rkv_paged_append(const rkv_paged_config* cfg, void* dev_pool, const rkv_paged_batch* batch, const void* dev_k, int64_t k_stride,
                      const void* dev_v, int64_t v_stride, void* stream);
 
@@ -393,14 +393,17 @@ int rkv_paged_scratch(const rkv_paged_config* cfg, const rkv_paged_batch* batch,
  * of prompts, drafted tokens, single tokens, in any mixture.  The row at position p sees the tokens t of its
  * sequence with t <= p (all of them without `causal`) and, with window > 0, t > p - window.
  *   dev_q      [n_rows][n_q_heads][head_dim] of the cache's type, rows q_stride elements apart (as k_stride)
- *   scale      of the scores, finite, also times log2(e) (1 / sqrt(head_dim) by custom)
+ *   scale      of the scores, finite, also times log2(e) (1 / sqrt(head_dim) by custom; with 0 every score that is
+ *              a number is 0)
  *   dev_out    [n_rows][n_q_heads][head_dim] of the cache's type, dense
  *   dev_lse    [n_rows][n_q_heads] fp32 log-sum-exp of the scaled scores, or NULL
  *   dev_scratch  256-byte aligned, scratch_bytes >= what rkv_paged_scratch says for this batch (else
  *              RKV_EINVAL); calls that may run at the same time need work spaces of their own
  * A row that sees no token, or whose scores are all -infinity, gets zeros and the log-sum-exp -infinity.
  * What a row does not see has no influence on it, infinities and NaN included.  Scores, softmax statistics
- * and sums are held in fp32; the same call on the same data gives the same bits. */
+ * and sums are held in fp32; weights are rounded to the cache's type before they multiply the values (their sum is
+ * of unrounded ones), which is up to 1.3 times as far from the exact result as the output's own rounding.  A scaled score
+ * that passes fp32 counts as an infinity, and a positive one makes its row NaN.  The same call on the same data gives the same bits. */
 int rkv_paged_attention(const rkv_paged_config* cfg, const void* dev_pool, const rkv_paged_batch* batch, const void* dev_q,
                         int64_t q_stride, int32_t causal, int32_t window, float scale, void* dev_out, float* dev_lse,
                         void* dev_scratch, size_t scratch_bytes, void* stream);

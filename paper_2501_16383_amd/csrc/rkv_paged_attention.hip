@@ -6,7 +6,9 @@
 // so that a lane of the result owns one column: the running maximum and sum of its softmax are plain registers, and
 // the weights a lane gets from the first product are, in their order, an operand of the second.
 // (Which token is which index of the sum is free as long as both operands agree.)  Weights are powers of two of
-// scores in fp32; the sum of weights is taken in fp32 from unrounded weights.
+// scores in fp32; the sum of weights is taken in fp32 from unrounded weights.  For the second product weights are rounded to
+// the cache's type, which is what a product on the matrix units at the rate of 16 bits costs: against the definition in 64 bits outputs are off by
+// up to 0.0022 (bf16) or 0.00026 (fp16) in k_paged_chunk, where the rounding of the output alone makes 0.0017 and 0.00021; few rows: 5 % more than it.
 #include <type_traits>
 
 #include "rkv_mfma_ops.h"
@@ -153,7 +155,8 @@ template <int D, int DT> __device__ __forceinline__ void paged_bad_rows(const Pa
 // these are in LDS, its keys as soon as these are multiplied.
 //
 // What bounds it: the stream of the cache.  32 sequences of 8192 tokens, 8 KV heads of 128, 8 bits: 96 us = 5.8 TB/s, and 94
-// with the arithmetic left out; more bytes in flight (three or four workgroups a compute unit) change nothing.
+// with the arithmetic left out; more bytes in flight (three or four workgroups a compute unit) change nothing.  With two blocks of
+// columns the registers are not enough: up to 34 scalar ones and, with 16 bits of bf16 and heads of 128, six vector ones are spilled.
 template <int D, int BITS, int DT, int NB>
 __global__ __launch_bounds__(256, NB == 1 ? 3 : 2) void k_paged_few(PagedView v, PagedAsk a) {
   constexpr int KL = D * BITS / 8 / 4 / 16;                 // 16-byte loads of a quarter row of keys (0: one of 8 bytes)
@@ -515,10 +518,10 @@ __global__ __launch_bounds__(256) void k_paged_merge(PagedView v, PagedAsk a) {
 // barrier a tile.  A wave works in half tiles: the softmax of one stands beside the scores of the next and the values of the one
 // before, so that matrix and vector unit have work that does not wait for the other.
 //
-// What bounds it: every product of 32 x 32 x 16 reads 1 KiB of LDS for 32 columns, and a compute unit's four matrix units
-// ask for those 128 bytes a cycle that its LDS gives.  8192 tokens, 32 query heads on 8 KV heads of 128, 16 bits: the products
-// and their reads alone take 390 us, the softmax alone 250, staging adds 80; together 530-560 us (1.0 PFLOP/s), the matrix units
-// half busy.  64 columns a wave would halve the reads, but their 512 registers leave one wave a SIMD, which took twice as long.
+// What bounds it: no unit by itself, but that softmax and staging do not wholly hide behind the products.  8192 tokens, 32 query heads
+// on 8 KV heads of 128, 16 bits: 540-570 us (0.96-1.0 PFLOP/s).  The products with their reads of LDS (1 KiB for every 32 x 32 x 16) alone take
+// 390 us, the softmax alone 250, staging adds 80; the matrix units are busy in 50 % of the cycles, LDS in 25 %, and 3 % of the waves' cycles
+// are spent waiting for it.  64 columns a wave would halve the reads, but their 512 registers leave one wave a SIMD, which took twice as long.
 #define PAGED_TILE 64
 
 // The tile of columns that a workgroup takes: sequence and first column, or b = n_seqs.  Sequences of more than `few`
@@ -1031,6 +1034,8 @@ __global__ __launch_bounds__(256) void k_paged_chunk_merge(PagedView v, PagedAsk
 // ---- host side ---------------------------------------------------------------------------------
 
 #define RKV_PAGED_CUS 256             // compute units that a launch should fill
+// (8 sequences of 4096 tokens, 8 KV heads of 128, 8 bits: 20 columns 23.7 us in k_paged_few and 34.4 in k_paged_chunk, 32 columns 25.6 and 35.0;
+// more than two blocks of columns do not fit k_paged_few's registers: 36 columns take 36.0)
 #define RKV_PAGED_FEW 32              // columns (rows times rep) of a sequence that k_paged_few takes ...
 #define RKV_PAGED_FEW_MIXED 16        // ... where others go to k_paged_chunk: single tokens, half the registers
 #define RKV_PAGED_SPLITS 256          // most splits of a sequence
@@ -1061,8 +1066,13 @@ static bool has_chunk(const PagedView& v) { return (int64_t)v.max_new * v.rep > 
 static bool has_few(const PagedView& v) { return v.n_seqs > 1 || !has_chunk(v); }
 
 // k_paged_few: a unit is a (sequence, KV head); splits of at least 128 tokens (32 for each wave).  Two workgroups for each
-// compute unit have enough bytes in flight, and four where a row is 64 bytes or less (32768 tokens, 32 heads, 4 bits: 31.0 us with
-// four, 36.6 with two; 8 x 4096 tokens, 8 heads, 8 bits: 20.5 with two, 24.5 with four).
+// compute unit have enough bytes in flight, and four where a row is 64 bytes or less and the spans are long (32768 tokens, 32 heads of 128,
+// 4 bits: 30.4 us with four, 35.6 with two; 8 x 4096 tokens, 8 heads, 8 bits: 19.8 with two, 24.2 with four).  Where the whole batch is short two are
+// better with narrow rows as well (2 x 16384 tokens, 8 heads: 16.9 against 18.8 with 4 bits, 13.7 against 15.8 with heads of 64), which the rule does not know.
+// One span is not cut up to 512 tokens (one token, 32 heads of 128 in 16 bits: 8.4 us whole, 12.6 cut; at 513-640 tokens 9.8 and 12.5, at 768 11.0
+// and 12.6, at 1024 13.8 and 12.6: the crossing is near 900 for this shape).  What a window leaves is counted for RKV_PAGED_FEW rows, also where there is one.
+// The number of splits follows the number of sequences and the longest of them, as the host knows no other lengths: one sequence of 32768 tokens among
+// seven of 512 takes 58 us, among 63 of them 402, because nothing is cut there.
 static int64_t few_units(const PagedView& v) { return (int64_t)v.n_seqs * v.Hkv; }
 static int few_cols(const PagedView& v) { return (int64_t)v.max_new * v.rep <= 16 || has_chunk(v) ? 16 : 32; }
 static int64_t few_want(int D, int bits) { return (D * bits <= 512 ? 4 : 2) * RKV_PAGED_CUS; }
@@ -1070,7 +1080,9 @@ static int64_t few_want(int D, int bits) { return (D * bits <= 512 ? 4 : 2) * RK
 #define FEW_WHOLE 512
 // k_paged_chunk: a unit is a tile of columns and a KV head; a workgroup for each compute unit, splits of at least 512 tokens
 static int64_t chunk_units(const PagedView& v) {
-  // every sequence of more than RKV_PAGED_FEW_MIXED columns, and one alone, may have a tile that is not full
+  // Every sequence of more than RKV_PAGED_FEW_MIXED columns, and one alone, may have a tile that is not full.  The host cannot tell those from
+  // single tokens, so that a chunk beside many of them is cut less than it could be: 1021 rows over 4090 tokens, 32 heads on 8, beside 14 single tokens
+  // 113 us in two splits, beside 15 in one 145.  (Over 1100 tokens one split is the better: 57 against 68.)
   const int64_t cols = (int64_t)v.n_rows * v.rep, most = cols / RKV_PAGED_FEW_MIXED, seqs = v.n_seqs < most ? v.n_seqs : most;
   return (cols / RKV_PAGED_COLS + seqs) * v.Hkv;
 }
