@@ -64,7 +64,7 @@ template <int DT> __device__ __forceinline__ uint32_t paged_times_zero(uint32_t 
 __device__ __forceinline__ float paged_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Weights are held times a power of two that the division by their sum takes out again: in fp16 the largest is
-// 2^14, so that one of 2^-28 of it still is a normal number (as a subnormal of 2^-25 it would be off by up to its own size).
+// 2^14 or a little more, so that one of 2^-28 of it still is a normal number (as a subnormal of 2^-25 it would be off by up to its own size).
 template <int DT> __device__ constexpr float paged_bias() { return DT ? 0.f : 14.f; }
 
 // The exponent that weights are taken against where the largest score's is `top`.  From 2^24 on fp32's numbers lie 2 and more
@@ -73,6 +73,10 @@ template <int DT> __device__ __forceinline__ float paged_ref(float top) {
   const float r = top - paged_bias<DT>();
   return top - r > 15.f ? top : r;
 }
+
+// ... and how far the largest may pass that before it is taken anew.  The difference is exact where it matters; half a power more than
+// the bias, because top - 14 is rounded and would look passed again and again.
+template <int DT> __device__ constexpr float paged_slack() { return DT ? 0.f : 14.5f; }
 
 // The exponent of the same power in k_paged_chunk, where weights may pass the largest by 2^8
 template <int DT> __device__ constexpr float paged_chunk_bias() { return DT ? 0.f : 6.f; }
@@ -350,8 +354,9 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 2) void k_paged_few(PagedView v,
       }
       float top = fmaxf(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])), fmaxf(fmaxf(w[4], w[5]), fmaxf(w[6], w[7])));
       top = paged_max4(top);
-      if (__any(top - paged_bias<DT>() > m[c])) {
-        const float m2 = fmaxf(m[c], paged_ref<DT>(top)), f = m2 == m[c] ? 1.f : paged_exp2(m[c] - m2);
+      const bool up = top - m[c] > paged_slack<DT>();
+      if (__any(up)) {
+        const float m2 = up ? paged_ref<DT>(top) : m[c], f = up ? paged_exp2(m[c] - m2) : 1.f;   // (of other columns nothing changes)
         m[c] = m2;
         l[c] *= f;
 #pragma unroll

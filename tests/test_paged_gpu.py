@@ -427,6 +427,32 @@ def test_scores_so_large_that_fp32_holds_few_of_them(bits, dtype, D, e, scale, n
     assert np.array_equal(a[0][few].cpu().double().numpy(), out[few.numpy()])
 
 
+@pytest.mark.parametrize("news", [[1, 1], [12, 1], [40, 1]], ids=str)
+@pytest.mark.parametrize("step", [1, 2, 3, 4])
+@pytest.mark.parametrize("dtype,e", [("fp16", 22), ("fp16", 24), ("fp16", 25), ("fp16", 26), ("fp16", 27), ("fp16", 28), ("bf16", 27)])
+def test_large_scores_that_grow(dtype, e, step, news):
+    """As above, the scores growing by `step` of fp32's neighbours every 128 tokens, so that every tile of a wave has a new maximum just above the
+    one before; up to 512 tokens, which one workgroup walks."""
+    lens = [500, 512]
+    s = Setup(lens, hq=2, hkv=1, D=64, bits=16, dtype=dtype, seed=e)
+    for k in s.k:
+        k.zero_()
+        k[:, 0, 0] = 2.0 ** (e - e // 2)
+        k[:, 0, 40] = torch.arange(k.shape[0]).div(128, rounding_mode="floor").to(k.dtype) * step
+    s.fill()
+    q = torch.zeros(sum(news), 2, 64, dtype=TYPES[dtype])
+    q[..., 0], q[..., 40] = 2.0 ** (e // 2), 2.0 ** (e - 23)
+    out, lse = (x.cpu().double().numpy() for x in s.cache.attention(q.to(DEV), s.batch(lens, news, max_len=512), scale=np.log(2), want_lse=True))
+    u, least = (2.0**-11, 2.0**-25) if dtype == "fp16" else (2.0**-8, 0)
+    row = 0
+    for b, (n, m) in enumerate(zip(lens, news)):
+        ref, rl, spread, _, mass = O.attention(q[row:row + m].double().numpy(), s.held(s.k, b, n), s.held(s.v, b, n), n - m, scale=np.log(2))
+        tol = spread * (u + (n + 16) * 2.0**-24) * 1.001 + u * np.abs(ref) + 2.0**-25 + mass * least
+        assert np.isfinite(out[row:row + m]).all() and (np.abs(out[row:row + m] - ref) <= tol).all(), b
+        assert (np.abs(lse[row:row + m] - rl) <= np.abs(rl) * 2.0**-22).all()
+        row += m
+
+
 def test_large_scores_and_what_is_no_number():
     """Rows whose scores are large, over a page outside the pool, a NaN key and an infinite one: NaN from there on, and the rows in front
     and the other KV head's as they are without."""
