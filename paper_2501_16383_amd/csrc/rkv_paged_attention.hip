@@ -525,7 +525,7 @@ __global__ __launch_bounds__(256) void k_paged_merge(PagedView v, PagedAsk a) {
 //
 // What bounds it: no unit by itself, but that softmax and staging do not wholly hide behind the products.  8192 tokens, 32 query heads
 // on 8 KV heads of 128, 16 bits: 540-570 us (0.96-1.0 PFLOP/s).  The products with their reads of LDS (1 KiB for every 32 x 32 x 16) alone take
-// 390 us, the softmax alone 250, staging adds 80; the matrix units are busy in 50 % of the cycles, LDS in 25 %, and 3 % of the waves' cycles
+// 390 us, the softmax alone 250, staging adds 80; the matrix units are busy in 51 % of the cycles, LDS in 26 %, and 3 % of the waves' cycles
 // are spent waiting for it.  64 columns a wave would halve the reads, but their 512 registers leave one wave a SIMD, which took twice as long.
 #define PAGED_TILE 64
 
